@@ -1,0 +1,435 @@
+"""What a paged server does before the first decode step, as operators: from the requests' lengths to an int4 cache.
+
+`tq_pages_append` gives every new token a place in the pool of pages, `tq_sdpa_prefill` attends the packed prompts,
+`tq_quantize_kv_slots` stores their K and V, and `tq_pages_trim` takes back the pages of sequences that end or get shorter.
+`run` calls them where `own` is true and evaluates the same definitions with elementary torch operations where it is false.
+
+A case is one call as a serving program makes it: the projections' output, the cache and the page state are on the GPU.
+"""
+import math
+
+import torch
+
+own = False
+
+
+# ---- the cases ------------------------------------------------------------------------------------------------
+
+def _prefill(name, lens, n_q_heads, n_kv_heads, head_dim, dtype, fused, window=0):
+    """lens: the sequences' lengths as text, "173" or "17-2048*24" (24 lengths of that range, spread over its logarithm)."""
+    return {"name": name, "kind": "prefill", "lens": lens, "n_q_heads": n_q_heads, "n_kv_heads": n_kv_heads,
+            "head_dim": head_dim, "dtype": dtype, "fused": fused, "window": window}
+
+
+def _store(name, lens, n_q_heads, n_kv_heads, head_dim, dtype, fused, group, page):
+    return {"name": name, "kind": "store", "lens": lens, "n_q_heads": n_q_heads, "n_kv_heads": n_kv_heads,
+            "head_dim": head_dim, "dtype": dtype, "fused": fused, "group": group, "page": page}
+
+
+def _append(name, batch, held, prompts, prompt, page, pool=100):
+    """batch sequences with "lo-hi" tokens in the cache take one more each; in place of the first `prompts` of them stand
+    prompts of "lo-hi" tokens that the cache does not hold yet.  pool: the free pages, as a share of what they take together."""
+    return {"name": name, "kind": "append", "batch": batch, "held": held, "prompts": prompts, "prompt": prompt, "page": page,
+            "pool": pool}
+
+
+def _trim(name, batch, held, ended, cut, page):
+    """batch sequences with "lo-hi" tokens: `ended` of them are over, the others lose up to `cut` of their last tokens."""
+    return {"name": name, "kind": "trim", "batch": batch, "held": held, "ended": ended, "cut": cut, "page": page}
+
+
+def listed():
+    return [
+        # one short chat turn on the 70B attention shape: the smallest prompt, where latency counts
+        _prefill("prompt_chat", "173", 64, 8, 128, "float16", False),
+        # the largest: a document in one sequence, same shape
+        _prefill("prompt_16k", "16384", 64, 8, 128, "float16", False),
+        # a server's batch of prompts of very different lengths, straight out of the fused projection, in bfloat16
+        _prefill("prompts_packed24", "17-2048*24", 64, 8, 128, "bfloat16", True),
+        # local layers at head dimension 256: a sliding window of 1024 tokens
+        _prefill("prompt_local256", "5003-5003*2", 32, 16, 256, "float16", False, window=1024),
+        # global layers at head dimension 512: 32 query heads on one KV head
+        _prefill("prompt_global512", "4099", 32, 1, 512, "bfloat16", True),
+        # the chat turn's K and V into pages
+        _store("store_chat", "173", 64, 8, 128, "float16", False, 32, 64),
+        # packed prompts out of the fused projection into pages: bulk quantising, bound by memory
+        _store("store_packed", "900-16000*8", 64, 8, 128, "float16", True, 32, 256),
+        # head dimension 256 in groups of 64, bfloat16, one prompt
+        _store("store_d256_g64", "20011", 32, 16, 256, "bfloat16", False, 64, 64),
+        # every decode step of 256 sequences: one token each, a new page now and then
+        _append("append_step256", 256, "64-4096", 0, "0-0", 64),
+        # a step that takes 24 prompts in next to 104 sequences that decode
+        _append("append_prompts", 128, "64-4096", 24, "500-12000", 256),
+        # after speculative verification: up to 7 rejected tokens to a sequence, a few of the 64 sequences over
+        _trim("trim_verify64", 64, "64-8192", 3, 7, 64),
+        # many long sequences end together: 45 thousand pages back
+        _trim("trim_ended512", 512, "1000-16000", 512, 0, 64),
+    ]
+
+
+HEADS = {128: [(8, 1), (32, 8), (64, 8), (64, 8), (128, 8), (32, 32), (24, 8)], 256: [(16, 8), (32, 16), (32, 4)],
+         512: [(32, 1), (16, 2)]}
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case: kinds, shapes, types and lengths of the listed ones, at most as large as the largest."""
+    kind = rng.choice(["prefill", "prefill", "prefill", "prefill", "store", "store", "append", "append", "trim"])
+    if kind in ("prefill", "store"):
+        dim = rng.choice([128, 128, 128, 256, 256, 512])
+        n_q, n_kv = rng.choice(HEADS[dim])
+        dtype, fused = rng.choice(["float16", "bfloat16"]), rng.random() < 0.5
+        count = rng.choice([1, 1, 1, _log(rng, 2, 64)])
+        if kind == "store":
+            top = int(120000 * 16 * 128 / (n_kv * dim * 2) / count)
+            hi = _log(rng, 16, max(32, min(65536, top)))
+            return _store("", _spread(rng, hi, count), n_q, n_kv, dim, dtype, fused,
+                          rng.choice([32, 32, 32, 64, 128]), rng.choice([64, 256]))
+        # pairs of query and key times heads times head_dim, at most half of the largest listed case's
+        top = int(math.sqrt(0.5 * 16384 * 16384 * 64 * 128 / (n_q * dim) / count))
+        hi = _log(rng, 16, min(16384, max(32, top)))
+        return _prefill("", _spread(rng, hi, count), n_q, n_kv, dim, dtype, fused, 1024 if dim == 256 and rng.random() < 0.7 else 0)
+    batch, page = _log(rng, 1, 768), rng.choice([32, 64, 256])
+    lo = _log(rng, 1, 4000)
+    held = "%d-%d" % (lo, _log(rng, lo, 16000))
+    if kind == "trim":
+        return _trim("", batch, held, rng.choice([0, batch, rng.randint(0, batch)]), rng.choice([0, 7, 1000]), page)
+    prompts = rng.choice([0, min(batch, _log(rng, 1, 32))])
+    lo = _log(rng, 1, 1000)
+    return _append("", batch, held, prompts, "%d-%d" % (lo, _log(rng, lo, 12000)), page, rng.choice([100, 100, 100, 40]))
+
+
+def _spread(rng, hi, count):
+    return str(hi) if count == 1 else "%d-%d*%d" % (max(1, hi // 64), hi, count)
+
+
+def _lens(text, seed):
+    """The lengths that a case's text stands for.  (Work goes by them, so they do not change with the inputs' seed.)"""
+    if "-" not in text:
+        return [int(text)]
+    span, _, count = text.partition("*")
+    lo, hi = (int(x) for x in span.split("-"))
+    gen = torch.Generator().manual_seed(seed)
+    at = torch.rand(int(count or 1), generator=gen, dtype=torch.float64)
+    return [int(x) for x in (math.log(max(lo, 1)) + at * (math.log(max(hi, 1)) - math.log(max(lo, 1)))).exp().round()]
+
+
+def _device():
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+# ---- inputs ---------------------------------------------------------------------------------------------------
+
+def _scale(case):
+    return 1.0 / math.sqrt(128) if case["head_dim"] == 128 else 1.0
+
+
+def _qkv(case, seed):
+    """q, k, v as the projections leave them: [tokens][heads][head_dim], each dense or all three out of one row per token.
+    The distributions are the library's synthetic ones: N(0, 1) with four outlier key channels to a head at head dimension 128,
+    N(0, 0.1^2) for q and k elsewhere."""
+    dev = _device()
+    gen = torch.Generator(device=dev).manual_seed(seed)
+    n, hq, hkv, d = sum(_lens(case["lens"], 7)), case["n_q_heads"], case["n_kv_heads"], case["head_dim"]
+    dtype = getattr(torch, case["dtype"])
+    std = torch.ones(hq + 2 * hkv, d)
+    if d == 128:
+        host = torch.Generator().manual_seed(seed + 17)
+        for h in range(hkv):
+            std[hq + h, torch.randperm(d, generator=host)[:4]] = 8.0
+    else:
+        std[:hq + hkv] = 0.1
+    row = torch.empty((n, hq + 2 * hkv, d), dtype=dtype, device=dev)
+    std = std.to(dev)
+    for at in range(0, n, 4096):
+        piece = row[at:at + 4096]
+        piece.copy_(torch.randn(piece.shape, generator=gen, device=dev) * std)
+    q, k, v = row[:, :hq], row[:, hq:hq + hkv], row[:, hq + hkv:]
+    return (q, k, v) if case["fused"] else (q.contiguous(), k.contiguous(), v.contiguous())
+
+
+def _slots_of(lens, page, seed):
+    """Pages out of a pool in random order for sequences of these lengths: the pool's page count, every token's slot."""
+    blocks = [-(-n // page) for n in lens]
+    order = torch.randperm(sum(blocks) + 3, generator=torch.Generator().manual_seed(seed + 5))
+    first = 0
+    slots = []
+    for n, b in zip(lens, blocks):
+        at = torch.arange(n)
+        slots.append(order[first + at // page] * page + at % page)
+        first += b
+    return sum(blocks) + 3, torch.cat(slots).to(torch.int32)
+
+
+def _held(case):
+    return _lens("%s*%d" % (case["held"], case["batch"]), 11)
+
+
+def _new_lens(case):
+    new = [1] * case["batch"]
+    new[:case["prompts"]] = _lens("%s*%d" % (case["prompt"], case["prompts"]), 13) if case["prompts"] else []
+    return new
+
+
+def _page_state(case, seed):
+    """Sequences in the middle of their life over a pool whose pages have been taken and given back in any order."""
+    page, held = case["page"], _held(case)
+    if case["kind"] == "append":
+        held[:case["prompts"]] = [0] * case["prompts"]
+        most = max(h + n for h, n in zip(held, _new_lens(case)))
+        spare = sum(-(-(h + n) // page) - -(-h // page) for h, n in zip(held, _new_lens(case)))
+        spare = spare * case["pool"] // 100 + (64 if case["pool"] == 100 else 0)
+    else:
+        most, spare = max(held), 64
+    blocks = torch.tensor([-(-h // page) for h in held])
+    max_blocks = -(-most // page) + 1
+    taken = int(blocks.sum())
+    order = torch.randperm(taken + spare, generator=torch.Generator().manual_seed(seed)).to(torch.int32)
+    table = torch.zeros((case["batch"], max_blocks), dtype=torch.int32)
+    table[torch.arange(max_blocks) < blocks.unsqueeze(1)] = order[:taken]
+    free = torch.zeros(taken + spare, dtype=torch.int32)
+    free[:spare] = order[taken:]
+    dev = _device()
+    return {"case": case, "page": page, "seq_lens": torch.tensor(held, dtype=torch.int32, device=dev), "block_table": table.to(dev),
+            "free_pages": free.to(dev), "n_free": torch.tensor([spare], dtype=torch.int32, device=dev),
+            "seq_lens_after": torch.zeros(case["batch"], dtype=torch.int32, device=dev),
+            "n_free_after": torch.zeros(1, dtype=torch.int32, device=dev)}
+
+
+def prepare(case, seed):
+    if case["kind"] == "append":
+        st = _page_state(case, seed)
+        new = _new_lens(case)
+        st["new_lens"] = torch.tensor(new, dtype=torch.int32, device=_device())
+        st["max_new_tokens"] = -(-sum(new) // 128) * 128                # (a bound, as a program with fixed buffers has)
+        return st
+    if case["kind"] == "trim":
+        st = _page_state(case, seed)
+        gen = torch.Generator().manual_seed(seed + 3)
+        held = torch.tensor(_held(case))
+        keep = (held - torch.randint(0, case["cut"] + 1, held.shape, generator=gen)).clamp(min=0)
+        keep[torch.randperm(case["batch"], generator=gen)[:case["ended"]]] = 0
+        st["keep_lens"] = keep.to(torch.int32).to(_device())
+        return st
+    q, k, v = _qkv(case, seed)
+    st = {"case": case, "k": k, "v": v}
+    lens = _lens(case["lens"], 7)
+    if case["kind"] == "prefill":
+        st["q"], st["scale"] = q, _scale(case)
+        st["cu_seqlens"] = torch.tensor([0] + lens).cumsum(0).to(torch.int32).to(_device())
+        st["lens"] = lens
+        return st
+    pages, slots = _slots_of(lens, case["page"], seed)
+    st["slots"] = slots.to(_device())
+    d, shape = case["head_dim"], (pages, case["n_kv_heads"], case["page"])
+    half = dict(dtype=torch.float16, device=_device())
+    for x in "kv":
+        st[x + "_codes"] = torch.zeros(shape + (d // 2,), dtype=torch.uint8, device=_device())
+        st[x + "_scale"] = torch.zeros(shape + (d // case["group"],), **half)
+        st[x + "_zero"] = torch.zeros(shape + (d // case["group"],), **half)
+    return st
+
+
+# ---- one pass -------------------------------------------------------------------------------------------------
+
+def _handle(st, make):
+    """The library's object over the program's tensors: made once, kept as long as they are."""
+    if "handle" not in st:
+        st["handle"] = make()
+    return st["handle"]
+
+
+def _run_own(st):
+    import paper_2604_16957_amd as tq
+    case = st["case"]
+    if case["kind"] == "prefill":
+        return tq.tq_sdpa_prefill(st["q"], st["k"], st["v"], st["cu_seqlens"], st["scale"], window=case["window"])
+    if case["kind"] == "store":
+        cache = _handle(st, lambda: tq.KVCache.wrap(st["k_codes"], st["k_scale"], st["k_zero"],
+                                                    st["v_codes"], st["v_scale"], st["v_zero"]))
+        tq.tq_quantize_kv_slots(cache, st["k"], st["v"], st["slots"])
+        return cache.tensors()
+    state = _handle(st, lambda: tq.PageState(st["seq_lens"], st["block_table"], st["free_pages"], st["n_free"], st["page"]))
+    if case["kind"] == "append":
+        cu_seqlens, slots, served = tq.tq_pages_append(state, st["new_lens"], st["max_new_tokens"],
+                                                       seq_lens_after=st["seq_lens_after"], n_free_after=st["n_free_after"])
+        return {"seq_lens": st["seq_lens_after"], "block_table": st["block_table"], "n_free": st["n_free_after"],
+                "cu_seqlens": cu_seqlens, "slots": slots, "served": served}
+    tq.tq_pages_trim(state, st["keep_lens"], seq_lens_after=st["seq_lens_after"], n_free_after=st["n_free_after"])
+    return {"seq_lens": st["seq_lens_after"], "free_pages": st["free_pages"], "n_free": st["n_free_after"]}
+
+
+def run(st):
+    if own:
+        return _run_own(st)
+    return {"prefill": _plain_prefill, "store": _plain_store, "append": _plain_append, "trim": _plain_trim}[st["case"]["kind"]](st)
+
+
+# A piece of the plain attention's score matrix is at most this many elements (8 GiB in 32 bits), which the card holds several of.
+SCORES = 1 << 31
+
+
+def _plain_prefill(st):
+    """softmax(scale q k^T, masked) v in 32 bits: one sequence at a time (they share no scores), as many heads at once as fit."""
+    case, q, k, v = st["case"], st["q"], st["k"], st["v"]
+    gqa = case["n_q_heads"] // case["n_kv_heads"]
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    first = 0
+    for n in st["lens"]:
+        rows = slice(first, first + n)
+        first += n
+        at = torch.arange(n, device=q.device)
+        back = at.unsqueeze(1) - at                                       # how many tokens the key lies behind the query
+        hidden = (back < 0) | (back >= case["window"]) if case["window"] else back < 0
+        step = max(1, min(case["n_kv_heads"], SCORES // (n * n * gqa)))
+        for h in range(0, case["n_kv_heads"], step):
+            kh = k[rows, h:h + step].permute(1, 2, 0).float().contiguous()
+            vh = v[rows, h:h + step].permute(1, 0, 2).float().contiguous()
+            qh = q[rows, h * gqa:(h + step) * gqa].permute(1, 0, 2).float().reshape(kh.shape[0], gqa * n, -1)
+            s = (torch.bmm(qh, kh) * st["scale"]).view(-1, gqa, n, n).masked_fill_(hidden, -math.inf)
+            p = (s - s.amax(-1, keepdim=True)).exp_()
+            del s
+            o = torch.bmm((p / p.sum(-1, keepdim=True)).view(-1, gqa * n, n), vh)
+            out[rows, h * gqa:(h + step) * gqa] = o.view(-1, n, o.shape[-1]).permute(1, 0, 2).to(q.dtype)
+    return out
+
+
+def _plain_quantize(x, group):
+    """Codes (two to a byte), scales and zero-points of rows [..., d]; quotients in 64 bits where the stored value hangs on the
+    last bit of one in 32."""
+    g = x.float().reshape(x.shape[:-1] + (-1, group))
+    mn, mx = g.amin(-1, keepdim=True), g.amax(-1, keepdim=True)
+    s = ((mx - mn).double() / 15.0).float().clamp(max=65504.0).half()
+    s = torch.where(s == 0, torch.ones_like(s), s)
+    z = ((-mn).double() / s.double()).float().clamp(-65504.0, 65504.0).half() + 0.0
+    code = ((g.double() / s.double()).float() + z.float()).round().clamp(0, 15).to(torch.uint8).reshape(x.shape)
+    return code[..., 0::2] | code[..., 1::2] << 4, s.squeeze(-1), z.squeeze(-1)
+
+
+def _plain_store(st):
+    page = st["slots"].long() // st["case"]["page"]
+    row = st["slots"].long() % st["case"]["page"]
+    for x in "kv":
+        codes, scale, zero = _plain_quantize(st[x], st["case"]["group"])
+        st[x + "_codes"][page, :, row] = codes
+        st[x + "_scale"][page, :, row] = scale
+        st[x + "_zero"][page, :, row] = zero
+    return tuple(st[x + part] for x in "kv" for part in ("_codes", "_scale", "_zero"))
+
+
+def _plain_append(st):
+    page, bound, table = st["page"], st["max_new_tokens"], st["block_table"]
+    max_blocks, free = table.shape[1], st["free_pages"]
+    have, want = st["seq_lens"].long().clamp(min=0), st["new_lens"].long().clamp(min=0)
+    n_free = st["n_free"].long().clamp(0, free.numel())
+    ends = want.cumsum(0)
+    held, reach = (have + page - 1) // page, (have + want + page - 1) // page
+    fits = (have + want <= max_blocks * page) & (ends <= bound)
+    need = torch.where(fits & (want > 0), reach - held, 0)
+    through = need.cumsum(0)
+    served = fits & ((need == 0) | (through <= n_free))
+    block = torch.arange(max_blocks, device=table.device)
+    new = served.unsqueeze(1) & (block >= held.unsqueeze(1)) & (block < reach.unsqueeze(1))
+    nth = (through - need).unsqueeze(1) + block - held.unsqueeze(1)       # this page is the nth from the stack's top
+    table = torch.where(new, free[(n_free - 1 - nth).clamp(0, free.numel() - 1)], table)
+    cu = torch.cat([ends.new_zeros(1), ends.clamp(max=bound)])
+    t = torch.arange(bound, device=table.device)
+    seq = torch.searchsorted(cu[1:], t, right=True).clamp(max=have.numel() - 1)
+    pos = have[seq] + t - cu[seq]
+    slot = table[seq, (pos // page).clamp(max=max_blocks - 1)].long() * page + pos % page
+    slots = torch.where((t < cu[-1]) & served[seq], slot, -1)
+    taken = torch.where(served, need, 0).sum()
+    return {"seq_lens": torch.where(served, have + want, have).to(torch.int32), "block_table": table,
+            "n_free": (n_free - taken).to(torch.int32), "cu_seqlens": cu.to(torch.int32), "slots": slots.to(torch.int32),
+            "served": served.to(torch.int32)}
+
+
+def _plain_trim(st):
+    page, table, free = st["page"], st["block_table"], st["free_pages"]
+    max_blocks = table.shape[1]
+    have = st["seq_lens"].long().clamp(min=0)
+    keep = torch.minimum(st["keep_lens"].long().clamp(min=0), have)
+    n_free = st["n_free"].long().clamp(0, free.numel())
+    held = ((have + page - 1) // page).clamp(max=max_blocks)
+    left = torch.minimum((keep + page - 1) // page, held)
+    block = torch.arange(max_blocks, device=table.device)
+    back = (block >= left.unsqueeze(1)) & (block < held.unsqueeze(1))
+    at = (n_free + back.view(-1).cumsum(0) - 1).view(back.shape)          # the stack's entry that this page becomes
+    back &= at < free.numel()
+    stack = torch.cat([free, free.new_zeros(1)])                          # (one more entry, for all that stay)
+    stack.scatter_(0, torch.where(back, at, free.numel()).view(-1), table.view(-1))
+    return {"seq_lens": keep.to(torch.int32), "free_pages": stack[:-1], "n_free": (n_free + back.sum()).to(torch.int32)}
+
+
+# ---- what a pass cannot do without ----------------------------------------------------------------------------
+
+def _pairs(n, window):
+    """Query and key pairs of a causal sequence of n tokens."""
+    w = min(n, window) if window else n
+    return w * (w + 1) // 2 + (n - w) * w
+
+
+def work(case):
+    if case["kind"] in ("prefill", "store"):
+        lens, hq, hkv, d = _lens(case["lens"], 7), case["n_q_heads"], case["n_kv_heads"], case["head_dim"]
+        if case["kind"] == "prefill":
+            return {"bytes": sum(lens) * (2 * hq + 2 * hkv) * d * 2,
+                    "flops": 4 * d * hq * sum(_pairs(n, case["window"]) for n in lens)}
+        return {"bytes": sum(lens) * (2 * hkv * (d * 2 + d // 2 + 4 * (d // case["group"])) + 4), "flops": 0}
+    page, held = case["page"], _held(case)
+    if case["kind"] == "append":
+        held[:case["prompts"]] = [0] * case["prompts"]
+        new = _new_lens(case)
+        pages = sum(-(-(h + n) // page) - -(-h // page) for h, n in zip(held, new))
+        slots = -(-sum(new) // 128) * 128
+        return {"bytes": 4 * (5 * case["batch"] + 2 * pages + slots + 3), "flops": 0}
+    pages = sum(-(-h // page) for h in held) * case["ended"] // case["batch"]
+    return {"bytes": 4 * (3 * case["batch"] + 2 * pages + 2), "flops": 0}
+
+
+# ---- the definition in 64 bits --------------------------------------------------------------------------------
+
+def exact(case, seed):
+    if case["kind"] in ("append", "trim"):
+        return None                                                       # whole numbers
+    lens = _lens(case["lens"], 7)
+    q, k, v = _qkv(case, seed)
+    if case["kind"] == "store":                                           # scale = range / 15; zero-point from the stored scale
+        pages, slots = _slots_of(lens, case["page"], seed)
+        at = slots.to(k.device).long()
+        outs = []
+        for x in (k, v):
+            g = x.double().reshape(x.shape[:-1] + (-1, case["group"]))
+            lo, span = g.amin(-1), (g.amax(-1) - g.amin(-1)) / 15.0
+            stored = span.float().clamp(max=65504.0).half().double()
+            stored = torch.where(stored == 0, torch.ones_like(stored), stored)
+            outs.append(None)
+            for value in (span, -lo / stored):
+                pool = value.new_zeros((pages * case["page"],) + value.shape[1:])
+                pool[at] = value
+                outs.append(pool.view((pages, case["page"]) + value.shape[1:]).transpose(1, 2).contiguous())
+        return tuple(outs)
+    gqa, window = case["n_q_heads"] // case["n_kv_heads"], case["window"]
+    out = torch.zeros(q.shape, dtype=torch.float64, device=q.device)
+    first = 0
+    for n in lens:
+        for h in range(case["n_kv_heads"]):
+            kd, vd = k[first:first + n, h].double(), v[first:first + n, h].double()
+            heads = slice(h * gqa, (h + 1) * gqa)
+            block = max(1, min(n, (1 << 28) // (n * gqa)))                # query tokens at a time
+            for lo in range(0, n, block):
+                hi = min(n, lo + block)
+                seen_from = max(0, lo - window + 1) if window else 0
+                x = q[first + lo:first + hi, heads].double().reshape(-1, kd.shape[1]) @ kd[seen_from:hi].t().contiguous()
+                own_at = torch.arange(lo, hi, device=q.device).repeat_interleave(gqa).unsqueeze(1)
+                key_at = torch.arange(seen_from, hi, device=q.device).unsqueeze(0)
+                mask = key_at > own_at
+                if window:
+                    mask |= key_at <= own_at - window
+                w = torch.softmax((x * _scale(case)).masked_fill(mask, -math.inf), dim=-1)
+                out[first + lo:first + hi, heads] = (w @ vd[seen_from:hi]).view(hi - lo, gqa, -1)
+        first += n
+    return out
