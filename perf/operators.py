@@ -327,8 +327,8 @@ def _plain_append(st):
     n_free = st["n_free"].long().clamp(0, free.numel())
     ends = want.cumsum(0)
     held, reach = (have + page - 1) // page, (have + want + page - 1) // page
-    fits = (have + want <= max_blocks * page) & (ends <= bound)
-    need = torch.where(fits & (want > 0), reach - held, 0)
+    fits = (have + want <= max_blocks * page) & ((want == 0) | (ends <= bound))
+    need = torch.where(fits, reach - held, 0)
     through = need.cumsum(0)
     served = fits & ((need == 0) | (through <= n_free))
     block = torch.arange(max_blocks, device=table.device)
