@@ -235,6 +235,94 @@ int tq_sdpa_int4_decode_paged(const tq_kv_cache* pool, const int32_t* block_tabl
                               void* out, void* workspace, size_t workspace_bytes,
                               const tq_decode_opts* opts, void* stream);
 
+/* ---- From a prompt to a paged cache (the S_q > 1 arm of Sec. 3.3: attend in 16 bits, quantise, store) ----
+ *
+ * Packed tokens: the new tokens of several sequences one after another, as the projections of a forward pass
+ * leave them.  q: [n_tokens][n_q_heads][head_dim], k, v: [n_tokens][n_kv_heads][head_dim], the heads of a token
+ * dense, `*_stride` elements from one token to the next (so that the three may be slices of one fused row; a
+ * stride is a multiple of 8, at least heads * head_dim, and below 2^24).  fp16 or bf16. */
+enum { TQ_DTYPE_F16 = 0, TQ_DTYPE_BF16 = 1 };
+
+typedef struct tq_packed_qkv {
+  const void* q;       /* may be NULL (and n_q_heads, q_stride 0) where only k and v are read */
+  const void* k;
+  const void* v;
+  int64_t q_stride, k_stride, v_stride;
+  int32_t n_tokens;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 128, 256 or 512 */
+  int32_t dtype;       /* TQ_DTYPE_* of q, k, v (and of out) */
+} tq_packed_qkv;
+
+/* Causal attention of whole prompts, before anything of them is quantised.  Sequence b is tokens
+ * [cu_seqlens[b], cu_seqlens[b + 1]) of the packed tokens; its token t attends its tokens 0 .. t, with window > 0 the
+ * last `window` of them (its own among them).  Query head h reads KV head h / (n_q_heads / n_kv_heads).
+ * out: [n_tokens][n_q_heads][head_dim], dense, of the inputs' type; it overlaps none of them.  fp32 scores, softmax and accumulation;
+ * the weights are rounded to the inputs' type in front of the product with V (and summed as rounded).
+ * cu_seqlens: DEVICE int32 [n_seqs + 1], ascending, read by the kernel; sequences may be empty.  Rows of out that no
+ * sequence has (before cu_seqlens[0], from cu_seqlens[n_seqs] on) are left as they are.  The values are clamped to
+ * [0, n_tokens], so that a bad one gives undefined rows of out but no access outside the arrays.
+ * attn_scale: any finite value.  No workspace; one launch.
+ * Errors: NULL, SHAPE, EMPTY (n_tokens or n_seqs < 1), UNSUPPORTED (dtype, window < 0, attn_scale not finite, 2^23
+ * blocks or more: n_tokens * n_q_heads / 128 + n_seqs * n_kv_heads), ALIGN, HIP. */
+int tq_sdpa_prefill(const tq_packed_qkv* x, const int32_t* cu_seqlens, int32_t n_seqs, float attn_scale,
+                    int32_t window, void* out, void* stream);
+
+/* Quantise and store packed tokens (Sec. 2.1, Eq. 2-3), each at a place of its own: token i goes to slot slots[i],
+ * i.e. to row slots[i] % capacity of cache row (page, or sequence of a contiguous cache) slots[i] / capacity.
+ * slots: DEVICE int32 [n_tokens], read by the kernel; a token whose slot is negative or past the cache
+ * is not stored.  Two tokens of a call must not have the same slot.  The same stored bits as tq_quantize_kv gives the same values; from bf16, whose range is wider
+ * than the stored fp16, the scale saturates at 65504 (as the zero-point does in any case).  x->q is not read.
+ * Any capacity >= 1 (the paged decode calls want a power of two >= 32).
+ * Errors: NULL, SHAPE (also x->n_kv_heads or head_dim unlike the cache's), EMPTY (n_tokens < 1),
+ * CAPACITY (batch * capacity > 2^31 - 1), UNSUPPORTED (dtype), ALIGN, HIP. */
+int tq_quantize_kv_slots(const tq_kv_cache* cache, const tq_packed_qkv* x, const int32_t* slots, void* stream);
+
+/* The bookkeeping of a paged cache, kept on the device: which pages of the pool (tq_kv_cache of n_pages pages of
+ * page_tokens tokens) each sequence holds, and which are free.  Sequence b holds seq_lens[b] tokens in its first
+ * ceil(seq_lens[b] / page_tokens) entries of block_table[b]; the other entries mean nothing.  free_pages is a
+ * stack: entries [0, *n_free) name the free pages, the last of them is taken first.  All arrays are the caller's
+ * and device int32, aligned to 4 bytes. */
+typedef struct tq_page_state {
+  int32_t* seq_lens;     /* [batch] */
+  int32_t* block_table;  /* [batch][max_blocks] */
+  int32_t* free_pages;   /* [n_pages] */
+  int32_t* n_free;       /* [1] */
+  int32_t batch;         /* at most TQ_MAX_PAGED_BATCH */
+  int32_t max_blocks;
+  int32_t n_pages;
+  int32_t page_tokens;   /* >= 1 (the paged decode calls want a power of two >= 32) */
+} tq_page_state;
+#define TQ_MAX_PAGED_BATCH 4096
+
+/* Room for new tokens: sequence b asks for new_lens[b] of them (0 or less: none).  In the order of the sequences, each takes
+ * the pages that it needs beyond those it holds from the top of the stack.  A sequence is served if its
+ * tokens fit into max_blocks pages, lie below max_new_tokens in the packed order, and the stack holds its pages and those of every sequence
+ * before it that the first two conditions do not exclude (nobody overtakes a sequence that waits for pages; one that needs none is served all
+ * the same).
+ *   cu_seqlens [batch + 1]: where each sequence's tokens lie in the packed order, served or not, no entry above max_new_tokens;
+ *   slots [max_new_tokens]: the slot of every packed token (for tq_quantize_kv_slots): -1 for tokens of a sequence
+ *     that is not served, from cu_seqlens[batch] on, and where a page's number is not one of the pool;
+ *   served [batch]: 1 or 0 (a sequence that asks for nothing is served as long as what it holds fits);
+ *   seq_lens_after [batch], n_free_after [1]: the lengths with the new tokens of the served, and what is left of the
+ *     stack.  They may be state->seq_lens and state->n_free themselves: the state is then brought forward in place.
+ * state->block_table gets the new pages' entries; state->free_pages is only read.  Negative lengths count as 0, *n_free is
+ * clamped to [0, n_pages].  new_lens overlaps no output.
+ * One launch, or two (in place, and more than 4096 new tokens).  Errors: NULL, SHAPE, EMPTY (max_new_tokens < 1), CAPACITY
+ * (n_pages * page_tokens or max_new_tokens > 2^31 - 2), UNSUPPORTED (batch > TQ_MAX_PAGED_BATCH), ALIGN, HIP. */
+int tq_pages_append(const tq_page_state* state, const int32_t* new_lens, int32_t max_new_tokens,
+                    int32_t* seq_lens_after, int32_t* n_free_after, int32_t* cu_seqlens, int32_t* slots,
+                    int32_t* served, void* stream);
+
+/* The way back: sequence b keeps its first keep_lens[b] tokens (0 or less: it is over; its length or more: it stays as it
+ * is), and the pages behind them go onto the stack, in the order of the sequences and of their blocks.  Rejected
+ * tokens of a speculative step, sequences that end or are preempted.  Entries of the block table are not changed.  Pages that would not fit
+ * onto the stack (n_pages entries; the state is then wrong) are dropped.  *_after as above.
+ * One launch, or two (in place, and more than 16384 entries in the block table).  Errors as above. */
+int tq_pages_trim(const tq_page_state* state, const int32_t* keep_lens, int32_t* seq_lens_after,
+                  int32_t* n_free_after, void* stream);
+
 /* The two phases of Sec. 3.2, separately callable (used for per-kernel timing).
  * partial: every chunk c writes (o_c, m_c, l_c) for each query head into workspace and
  * *n_splits_out (host int, may be NULL) receives the chunk count used.  reduce: merges

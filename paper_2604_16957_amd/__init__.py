@@ -5,6 +5,7 @@ libtq_mi355x.so.  PyTorch is used for device memory and streams, nothing else.
 """
 from .binding import (  # noqa: F401
     KVCache,
+    PageState,
     TqError,
     library_path,
     tq_decode_launches,
@@ -12,9 +13,12 @@ from .binding import (  # noqa: F401
     tq_dequant_then_attend,
     tq_kv_bytes,
     tq_kv_bytes_grouped,
+    tq_pages_append,
+    tq_pages_trim,
     tq_plan_splits,
     tq_quantize_kv,
     tq_quantize_kv_paged,
+    tq_quantize_kv_slots,
     tq_quantize_kv_varlen,
     tq_sdpa_int4_append_decode,
     tq_sdpa_int4_append_decode_paged,
@@ -25,6 +29,7 @@ from .binding import (  # noqa: F401
     tq_sdpa_int4_decode_varlen,
     tq_sdpa_int4_partial,
     tq_sdpa_int4_reduce,
+    tq_sdpa_prefill,
     tq_status_string,
     tq_workspace_bytes,
     raw,

@@ -28,6 +28,17 @@ class TqDecodeOptsStruct(ctypes.Structure):
                 ("n_queries", ctypes.c_int32)]
 
 
+class TqPackedStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v")] + \
+               [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + \
+               [(n, ctypes.c_int32) for n in ("n_tokens", "n_q_heads", "n_kv_heads", "head_dim", "dtype")]
+
+
+class TqPageStateStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("seq_lens", "block_table", "free_pages", "n_free")] + \
+               [(n, ctypes.c_int32) for n in ("batch", "max_blocks", "n_pages", "page_tokens")]
+
+
 class TqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -69,6 +80,11 @@ def raw():
         for f in (L.tq_quantize_kv, L.tq_sdpa_int4_decode, L.tq_sdpa_int4_partial, L.tq_sdpa_int4_reduce,
                   L.tq_dequant_then_attend):
             f.restype = ctypes.c_int
+        XP, SP = ctypes.POINTER(TqPackedStruct), ctypes.POINTER(TqPageStateStruct)
+        L.tq_sdpa_prefill.argtypes = [XP, P, I, F, I, P, P]
+        L.tq_quantize_kv_slots.argtypes = [CP, XP, P, P]
+        L.tq_pages_append.argtypes = [SP, P, I, P, P, P, P, P, P]
+        L.tq_pages_trim.argtypes = [SP, P, P, P, P]
         L.tq_workspace_bytes.argtypes = [I, I, I]
         L.tq_workspace_bytes.restype = SZ
         L.tq_dense_scratch_bytes.argtypes = [I, I, I, I]
@@ -135,6 +151,25 @@ class KVCache:
         self.struct = TqKvCacheStruct(
             self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.k_zero.data_ptr(),
             self.v_scale.data_ptr(), self.v_zero.data_ptr(), batch, n_kv_heads, head_dim, group_size, capacity, 0)
+
+    @classmethod
+    def wrap(cls, k_codes, k_scale, k_zero, v_codes, v_scale, v_zero) -> "KVCache":
+        """A cache over six tensors that the program has already (in the order of `tensors()`): nothing is allocated or copied."""
+        self = cls.__new__(cls)
+        self.batch, self.n_kv_heads, self.capacity, half_dim = k_codes.shape
+        self.head_dim, n_groups = 2 * half_dim, k_scale.shape[-1]
+        self.group_size = self.head_dim // max(n_groups, 1)
+        for name, t in (("k_codes", k_codes), ("v_codes", v_codes), ("k_scale", k_scale), ("k_zero", k_zero),
+                        ("v_scale", v_scale), ("v_zero", v_zero)):
+            codes = name.endswith("codes")
+            _need(t, torch.uint8 if codes else torch.float16, name)
+            if t.shape != k_codes.shape[:3] + ((half_dim,) if codes else (n_groups,)) or t.device != k_codes.device:
+                raise ValueError(f"{name}: shape or device unlike the other tensors of the cache")
+            setattr(self, name, t)
+        self.struct = TqKvCacheStruct(
+            k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), k_zero.data_ptr(), v_scale.data_ptr(),
+            v_zero.data_ptr(), self.batch, self.n_kv_heads, self.head_dim, self.group_size, self.capacity, 0)
+        return self
 
     def tensors(self):
         return (self.k_codes, self.k_scale, self.k_zero, self.v_codes, self.v_scale, self.v_zero)
@@ -409,3 +444,141 @@ def tq_dequant_then_attend(cache: KVCache, q: torch.Tensor, seq_len: int, attn_s
                                       _opts(n_splits, variant), _stream_ptr(stream))
     _check(rc, "tq_dequant_then_attend")
     return out
+
+
+# ---- from a prompt to a paged cache ----------------------------------------------------------------------------
+
+_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+class PageState:
+    """Which pages of a pool each sequence holds, and which are free: four int32 device tensors of the caller's (the fields
+    of tq_page_state), read and brought forward by tq_pages_append and tq_pages_trim."""
+
+    def __init__(self, seq_lens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
+                 page_tokens: int):
+        for name, t, dim in (("seq_lens", seq_lens, 1), ("block_table", block_table, 2), ("free_pages", free_pages, 1),
+                             ("n_free", n_free, 1)):
+            _need(t, torch.int32, name)
+            if t.dim() != dim or t.device != seq_lens.device:
+                raise ValueError(f"{name}: expected {dim} dimension(s), on the device of seq_lens")
+        if block_table.shape[0] != seq_lens.shape[0] or n_free.numel() != 1:
+            raise ValueError("block_table must be [batch, max_blocks], seq_lens [batch], n_free [1]")
+        self.seq_lens, self.block_table, self.free_pages, self.n_free = seq_lens, block_table, free_pages, n_free
+        self.batch, self.max_blocks = (int(x) for x in block_table.shape)
+        self.n_pages, self.page_tokens = int(free_pages.shape[0]), int(page_tokens)
+        self.struct = TqPageStateStruct(seq_lens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), n_free.data_ptr(),
+                                        self.batch, self.max_blocks, self.n_pages, self.page_tokens)
+
+    @classmethod
+    def empty(cls, batch: int, max_blocks: int, n_pages: int, page_tokens: int, device="cuda") -> "PageState":
+        """No sequence holds anything, every page is free (page 0 is taken first)."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.zeros(batch, **i32), torch.zeros((batch, max_blocks), **i32),
+                   torch.arange(n_pages - 1, -1, -1, **i32), torch.full((1,), n_pages, **i32), page_tokens)
+
+
+def _on(device, stream):
+    """The stream of a call whose tensors are on `device`: the given one, or that device's current one.  A kernel is launched on
+    the calling thread's current device, so a call for another one is refused rather than sent to the wrong GPU."""
+    if _device_of_thread is not None and device.index != _device_of_thread():
+        raise ValueError(f"the tensors are on {device}, which is not the current device: call under torch.cuda.device({device.index})")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device.index)
+    return _stream_ptr(stream)
+
+
+def _packed_rows(t: torch.Tensor, name: str, dtype, device) -> int:
+    """t: [tokens, heads, head_dim] with a token's heads dense; the elements from one token to the next."""
+    if not t.is_cuda or t.dtype != dtype or t.device != device or dtype not in _DTYPES:
+        raise TypeError(f"{name}: expected a CUDA tensor of float16 or bfloat16, all of one type and device")
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name}: expected [tokens, heads, head_dim] with a token's heads one after another")
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1] * t.shape[2])
+
+
+def _int32s(t: torch.Tensor, name: str, n: int, device):
+    if t.dtype != torch.int32 or t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous int32 tensor of {n} elements on {device}")
+
+
+def tq_sdpa_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, attn_scale: float,
+                    window: int = 0, out=None, stream=None) -> torch.Tensor:
+    """Causal attention of packed prompts: q fp16 or bf16 [T, H_q, d], k and v [T, H_kv, d] (slices of one fused row are fine),
+    cu_seqlens int32 [n_seqs + 1] on the device -> out [T, H_q, d].  Rows that no sequence has are left as they are in `out`
+    (undefined in one that the call makes)."""
+    dtype, device = q.dtype, q.device
+    qs, ks, vs = (_packed_rows(t, n, dtype, device) for t, n in ((q, "q"), (k, "k"), (v, "v")))
+    tokens, hq, d = q.shape
+    if k.shape != v.shape or k.shape[0] != tokens or k.shape[2] != d:
+        raise ValueError("k and v must be [tokens, n_kv_heads, head_dim] of q's tokens and head_dim")
+    _int32s(cu_seqlens, "cu_seqlens", cu_seqlens.numel(), device)
+    if out is None:
+        out = torch.empty((tokens, hq, d), dtype=dtype, device=device)
+    elif out.shape != q.shape or out.dtype != dtype or out.device != device or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape, type and device")
+    x = TqPackedStruct(q.data_ptr(), k.data_ptr(), v.data_ptr(), qs, ks, vs, tokens, hq, k.shape[1], d, _DTYPES[dtype])
+    rc = raw().tq_sdpa_prefill(ctypes.byref(x), cu_seqlens.data_ptr(), cu_seqlens.numel() - 1, float(attn_scale), int(window),
+                               out.data_ptr(), _on(device, stream))
+    _check(rc, "tq_sdpa_prefill")
+    return out
+
+
+def tq_quantize_kv_slots(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+    """k, v: fp16 or bf16 [T, H_kv, d] (slices of one fused row are fine); slots: int32 [T] on the device, token i goes to row
+    slots[i] % capacity of page (or sequence) slots[i] // capacity of the cache; negative: it is not stored."""
+    dtype, device = k.dtype, cache.k_codes.device
+    ks, vs = _packed_rows(k, "k", dtype, device), _packed_rows(v, "v", dtype, device)
+    tokens, heads, d = k.shape
+    if v.shape != k.shape:
+        raise ValueError("k and v must be of one shape")
+    _int32s(slots, "slots", tokens, device)
+    x = TqPackedStruct(None, k.data_ptr(), v.data_ptr(), 0, ks, vs, tokens, 0, heads, d, _DTYPES[dtype])
+    rc = raw().tq_quantize_kv_slots(ctypes.byref(cache.struct), ctypes.byref(x), slots.data_ptr(), _on(device, stream))
+    _check(rc, "tq_quantize_kv_slots")
+
+
+def _after(state: PageState, seq_lens_after, n_free_after):
+    """Where the state goes: the given tensors, or its own."""
+    lens = state.seq_lens if seq_lens_after is None else seq_lens_after
+    free = state.n_free if n_free_after is None else n_free_after
+    device = state.seq_lens.device
+    if lens is not state.seq_lens:
+        _int32s(lens, "seq_lens_after", state.batch, device)
+    if free is not state.n_free:
+        _int32s(free, "n_free_after", 1, device)
+    return lens.data_ptr(), free.data_ptr(), device
+
+
+def tq_pages_append(state: PageState, new_lens: torch.Tensor, max_new_tokens: int, seq_lens_after=None, n_free_after=None,
+                    cu_seqlens=None, slots=None, served=None, stream=None):
+    """Pages and slots for new_lens[b] (int32 [batch], device) new tokens of every sequence -> (cu_seqlens [batch + 1],
+    slots [max_new_tokens], served [batch]).  The state's block table gets the new pages; its lengths and free count are brought
+    forward in place, or, where seq_lens_after / n_free_after are given, written there."""
+    lens, free, device = _after(state, seq_lens_after, n_free_after)
+    _int32s(new_lens, "new_lens", state.batch, device)
+    i32 = dict(dtype=torch.int32, device=device)
+    if cu_seqlens is None:
+        cu_seqlens = torch.empty(state.batch + 1, **i32)
+    else:
+        _int32s(cu_seqlens, "cu_seqlens", state.batch + 1, device)
+    if slots is None:
+        slots = torch.empty(max(int(max_new_tokens), 0), **i32)
+    else:
+        _int32s(slots, "slots", int(max_new_tokens), device)
+    if served is None:
+        served = torch.empty(state.batch, **i32)
+    else:
+        _int32s(served, "served", state.batch, device)
+    rc = raw().tq_pages_append(ctypes.byref(state.struct), new_lens.data_ptr(), int(max_new_tokens), lens, free,
+                               cu_seqlens.data_ptr(), slots.data_ptr(), served.data_ptr(), _on(device, stream))
+    _check(rc, "tq_pages_append")
+    return cu_seqlens, slots, served
+
+
+def tq_pages_trim(state: PageState, keep_lens: torch.Tensor, seq_lens_after=None, n_free_after=None, stream=None) -> None:
+    """Sequence b keeps its first keep_lens[b] tokens (int32 [batch], device); the pages behind them go back on the stack."""
+    lens, free, device = _after(state, seq_lens_after, n_free_after)
+    _int32s(keep_lens, "keep_lens", state.batch, device)
+    rc = raw().tq_pages_trim(ctypes.byref(state.struct), keep_lens.data_ptr(), lens, free, _on(device, stream))
+    _check(rc, "tq_pages_trim")

@@ -582,6 +582,36 @@ int paged_view(const tq_kv_cache* pool, const int32_t* block_table, int32_t max_
   return TQ_OK;
 }
 
+// Packed tokens; need_q: q is read as well.  Everything but the alignment of pointers (TQ_ERR_ALIGN comes last in every call).
+int check_packed(const tq_packed_qkv* x, bool need_q) {
+  if (!x || !x->k || !x->v || (need_q && !x->q)) return TQ_ERR_NULL;
+  if (!head_dim_ok(x->head_dim) || x->n_kv_heads < 1) return TQ_ERR_SHAPE;
+  if (need_q && (x->n_q_heads < 1 || x->n_q_heads % x->n_kv_heads != 0)) return TQ_ERR_SHAPE;
+  auto stride_ok = [&](int64_t stride, int heads) {
+    return stride % 8 == 0 && stride >= (int64_t)heads * x->head_dim && stride < (1 << 24);
+  };
+  if (!stride_ok(x->k_stride, x->n_kv_heads) || !stride_ok(x->v_stride, x->n_kv_heads) ||
+      (need_q && !stride_ok(x->q_stride, x->n_q_heads)))
+    return TQ_ERR_SHAPE;
+  if (x->n_tokens < 1) return TQ_ERR_EMPTY;
+  if (x->dtype != TQ_DTYPE_F16 && x->dtype != TQ_DTYPE_BF16) return TQ_ERR_UNSUPPORTED;
+  return TQ_OK;
+}
+
+constexpr int64_t kMaxSlots = INT32_MAX - 1;      // (slots, and a page number past the last, are int32)
+
+int check_pages(const tq_page_state* st, const void* ask, const void* lens_after, const void* n_free_after) {
+  if (!st || !st->seq_lens || !st->block_table || !st->free_pages || !st->n_free || !ask || !lens_after || !n_free_after)
+    return TQ_ERR_NULL;
+  if (st->batch < 1 || st->max_blocks < 1 || st->n_pages < 1 || st->page_tokens < 1) return TQ_ERR_SHAPE;
+  if ((int64_t)st->n_pages * st->page_tokens > kMaxSlots) return TQ_ERR_CAPACITY;
+  if (st->batch > TQ_MAX_PAGED_BATCH) return TQ_ERR_UNSUPPORTED;
+  for (const void* p : {static_cast<const void*>(st->seq_lens), static_cast<const void*>(st->block_table), static_cast<const void*>(st->free_pages),
+                        static_cast<const void*>(st->n_free), ask, lens_after, n_free_after})
+    if (!aligned(p, 4)) return TQ_ERR_ALIGN;
+  return TQ_OK;
+}
+
 // ---- tq_sdpa_int4_decode_static: the workspace of callers that cannot allocate.
 // One array per GPU the library runs on, held until the process ends.  In host code the array's name is only a
 // stand-in for the symbol: the memory's address on a device is what hipGetSymbolAddress returns with that
@@ -972,6 +1002,50 @@ int tq_dequant_then_attend(const tq_kv_cache* cache, const void* q, int32_t n_q_
                       : tq::launch_partial_valu(p, cache->batch, cache->head_dim, true, s));
   if (rc != TQ_OK) return rc;
   return hip_rc(tq::launch_reduce(p, cache->batch, cache->head_dim, s));
+}
+
+int tq_sdpa_prefill(const tq_packed_qkv* x, const int32_t* cu_seqlens, int32_t n_seqs, float attn_scale, int32_t window,
+                    void* out, void* stream) {
+  const int rc = check_packed(x, true);
+  if (rc == TQ_ERR_NULL || !cu_seqlens || !out) return TQ_ERR_NULL;
+  if (rc != TQ_OK) return rc;
+  if (n_seqs < 1) return TQ_ERR_EMPTY;
+  if (window < 0 || !std::isfinite(attn_scale)) return TQ_ERR_UNSUPPORTED;
+  if (tq::prefill_blocks(*x, n_seqs) >= (1 << 23)) return TQ_ERR_UNSUPPORTED;   // (a grid has fewer than 2^32 threads)
+  if (!aligned(x->q, 16) || !aligned(x->k, 16) || !aligned(x->v, 16) || !aligned(out, 16) || !aligned(cu_seqlens, 4))
+    return TQ_ERR_ALIGN;
+  return hip_rc(tq::launch_prefill(*x, cu_seqlens, n_seqs, attn_scale, window, out, static_cast<hipStream_t>(stream)));
+}
+
+int tq_quantize_kv_slots(const tq_kv_cache* cache, const tq_packed_qkv* x, const int32_t* slots, void* stream) {
+  const int rc = check_cache(cache), rx = check_packed(x, false);
+  if (rc == TQ_ERR_NULL || rx == TQ_ERR_NULL || !slots) return TQ_ERR_NULL;
+  if (rc != TQ_OK && rc != TQ_ERR_ALIGN) return rc;
+  if (rx != TQ_OK) return rx;
+  if (x->n_kv_heads != cache->n_kv_heads || x->head_dim != cache->head_dim) return TQ_ERR_SHAPE;
+  if (x->n_kv_heads > 65535) return TQ_ERR_UNSUPPORTED;            // (a grid dimension)
+  if ((int64_t)cache->batch * cache->capacity > kMaxSlots) return TQ_ERR_CAPACITY;
+  if (rc == TQ_ERR_ALIGN || !aligned(x->k, 16) || !aligned(x->v, 16) || !aligned(slots, 4)) return TQ_ERR_ALIGN;
+  return hip_rc(tq::launch_quantize_slots(*cache, *x, slots, static_cast<hipStream_t>(stream)));
+}
+
+int tq_pages_append(const tq_page_state* state, const int32_t* new_lens, int32_t max_new_tokens, int32_t* seq_lens_after,
+                    int32_t* n_free_after, int32_t* cu_seqlens, int32_t* slots, int32_t* served, void* stream) {
+  const int rc = check_pages(state, new_lens, seq_lens_after, n_free_after);
+  if (rc == TQ_ERR_NULL || !cu_seqlens || !slots || !served) return TQ_ERR_NULL;
+  if (rc != TQ_OK && rc != TQ_ERR_ALIGN) return rc;
+  if (max_new_tokens < 1) return TQ_ERR_EMPTY;
+  if (max_new_tokens > kMaxSlots) return TQ_ERR_CAPACITY;
+  if (rc == TQ_ERR_ALIGN || !aligned(cu_seqlens, 4) || !aligned(slots, 4) || !aligned(served, 4)) return TQ_ERR_ALIGN;
+  return hip_rc(tq::launch_pages_append(*state, new_lens, max_new_tokens, seq_lens_after, n_free_after, cu_seqlens, slots, served,
+                                        static_cast<hipStream_t>(stream)));
+}
+
+int tq_pages_trim(const tq_page_state* state, const int32_t* keep_lens, int32_t* seq_lens_after, int32_t* n_free_after,
+                  void* stream) {
+  const int rc = check_pages(state, keep_lens, seq_lens_after, n_free_after);
+  if (rc != TQ_OK) return rc;
+  return hip_rc(tq::launch_pages_trim(*state, keep_lens, seq_lens_after, n_free_after, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -149,10 +149,13 @@ __device__ __forceinline__ float wave_fsum(float x) {
 // Sec. 2.1, Eq. 2-3.  Every fp32 step is a separately rounded operation (no contraction, correctly rounded
 // divides), so the bits are the same wherever this runs.
 // Eq. 2 from a group's min and max: s = (max - min) / 15 stored as fp16 (a scale that rounds to zero becomes
-// 1.0), z = -min / s from the STORED scale (saturated, never -0).
+// 1.0), z = -min / s from the STORED scale (saturated, never -0).  WIDE: min and max may lie outside fp16's range (bf16 input);
+// the scale then saturates as well.
+template <bool WIDE = false>
 __device__ inline void quantize_scale_zero(float mn, float mx, half_t& s16, half_t& z16) {
 #pragma clang fp contract(off)
-  const float s32 = __fdiv_rn(__fsub_rn(mx, mn), 15.0f);
+  float s32 = __fdiv_rn(__fsub_rn(mx, mn), 15.0f);
+  if (WIDE) s32 = fminf(s32, 65504.0f);
   s16 = (half_t)s32;
   if ((__builtin_bit_cast(uint16_t, s16) & 0x7FFFu) == 0) s16 = (half_t)1.0f;
   const float z32 = __fdiv_rn(__fsub_rn(0.0f, mn), (float)s16);
@@ -194,7 +197,8 @@ __device__ inline QuantFast quantize_fast_setup(float sf, float zf, float abs_ma
   return f;
 }
 __device__ inline bool quantize_fast_in_doubt(float far, const QuantFast& f) { return !(far < 0.5f - f.tol); }
-__device__ inline uint32_t quantize_word_fast(const half_t* x, const QuantFast& f, float& far) {
+template <typename T>
+__device__ inline uint32_t quantize_word_fast(const T* x, const QuantFast& f, float& far) {
 #pragma clang fp contract(off)
   // Adding 1.5 * 2^23 rounds a value of [0, 15] to an integer, half to even, and leaves that integer in the low
   // bits of the sum's encoding; eight encodings summed at 4-bit offsets carry the same known excess.
@@ -512,6 +516,14 @@ hipError_t launch_partial_wide(const DecodeParams& p, int batch, int head_dim, h
 hipError_t launch_reduce(const DecodeParams& p, int batch, int head_dim, hipStream_t s);
 // Whether the merge of that many outputs runs as one block per (output row, KV head).
 bool reduce_is_grouped(int head_dim, int64_t out_rows, int n_q_heads, int gqa);
+// Packed tokens (arguments checked): attention of prompts, quantise by slots, the page state's two ways.
+hipError_t launch_prefill(const tq_packed_qkv& x, const int32_t* cu_seqlens, int n_seqs, float attn_scale, int window, void* out,
+                          hipStream_t s);
+int64_t prefill_blocks(const tq_packed_qkv& x, int n_seqs);
+hipError_t launch_quantize_slots(const tq_kv_cache& c, const tq_packed_qkv& x, const int32_t* slots, hipStream_t s);
+hipError_t launch_pages_append(const tq_page_state& st, const int32_t* new_lens, int32_t max_new_tokens, int32_t* lens_after,
+                               int32_t* n_free_after, int32_t* cu_seqlens, int32_t* slots, int32_t* served, hipStream_t s);
+hipError_t launch_pages_trim(const tq_page_state& st, const int32_t* keep_lens, int32_t* lens_after, int32_t* n_free_after, hipStream_t s);
 
 }  // namespace tq
 

@@ -114,6 +114,74 @@ __global__ __launch_bounds__(256) void quantize_append_kernel(QuantParams p) {
   }
 }
 
+struct SlotsParams {
+  const void* src[2];     // k, v: [n_tokens] rows of `stride` elements, head h at h * D
+  int64_t stride[2];
+  uint8_t* codes[2];      // [rows][H_kv][capacity][D/2]
+  half_t* scale[2];       // [rows][H_kv][capacity][D/group]
+  half_t* zero[2];
+  const int32_t* slots;   // [n_tokens]
+  int32_t n_tokens, n_kv_heads, capacity, group;
+  uint32_t n_slots;       // cache rows * capacity
+};
+
+// Packed tokens to slots.  The thread's piece and its arithmetic are those of quantize_append_kernel; what differs is
+// who takes which piece: a block has consecutive tokens of ONE head (256 / (D / 32) of them), whose slots mostly follow each
+// other, so that it writes whole lines of codes, scales and zero-points, while a token's heads lie side by side in
+// the source only.  Bound by memory.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void quantize_slots_kernel(SlotsParams p) {
+  constexpr int NG = D / kGroup;                      // 32-element pieces per vector
+  constexpr bool kWide = sizeof(T) == 2 && !__is_same(T, half_t);
+  const int which = blockIdx.z, h = blockIdx.y, g = threadIdx.x % NG;
+  const int64_t t = (int64_t)blockIdx.x * (256 / NG) + threadIdx.x / NG;
+  if (t >= p.n_tokens) return;
+  const uint32_t slot = p.slots[t];                   // (a negative one is past the cache as well)
+  union Pack { uint4 v; T x[8]; } u[4];
+  const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const T*>(p.src[which]) + t * p.stride[which] + h * D + g * kGroup);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i].v = src[i];
+  if (slot >= p.n_slots) return;                      // (all pieces of a vector: neighbouring lanes that exchange below)
+  float mn = (float)u[0].x[0], mx = mn;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      mn = fminf(mn, (float)u[i].x[j]);
+      mx = fmaxf(mx, (float)u[i].x[j]);
+    }
+  }
+  const int pieces = p.group / kGroup;                // 1, 2 or 4
+  for (int off = 1; off < pieces; off <<= 1) {
+    mn = fminf(mn, __shfl_xor(mn, off));
+    mx = fmaxf(mx, __shfl_xor(mx, off));
+  }
+  half_t s16, z16;
+  quantize_scale_zero<kWide>(mn, mx, s16, z16);
+  const float sf = (float)s16, zf = (float)z16;
+  uint32_t w[4];
+  const QuantFast fast = quantize_fast_setup(sf, zf, fmaxf(fabsf(mn), fabsf(mx)));
+  float far = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = quantize_word_fast(u[i].x, fast, far);
+  if (quantize_fast_in_doubt(far, fast)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = (float)u[i].x[j];
+      w[i] = quantize_word(x, sf, zf);
+    }
+  }
+  const uint32_t page = slot / (uint32_t)p.capacity;
+  const int64_t row = ((int64_t)page * p.n_kv_heads + h) * p.capacity + (slot - page * (uint32_t)p.capacity);
+  store_stream16(p.codes[which] + row * (D / 2) + g * (kGroup / 2), w[0], w[1], w[2], w[3]);
+  if (g % pieces == 0) {
+    p.scale[which][row * (NG / pieces) + g / pieces] = s16;
+    p.zero[which][row * (NG / pieces) + g / pieces] = z16;
+  }
+}
+
 struct DequantParams {
   const uint8_t* codes[2];
   const half_t* scale[2];
@@ -177,6 +245,38 @@ hipError_t launch_quantize(const tq_kv_cache& c, const void* k_new, const void* 
   p.groups_per_tensor = (int64_t)batch * c.n_kv_heads * n_new * (c.head_dim / kGroup);
   const unsigned blocks = (unsigned)((p.groups_per_tensor + 255) / 256);
   hipLaunchKernelGGL(quantize_append_kernel, dim3(blocks, 2), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_quantize_slots(const tq_kv_cache& c, const tq_packed_qkv& x, const int32_t* slots, hipStream_t s) {
+  SlotsParams p;
+  p.src[0] = x.k;
+  p.src[1] = x.v;
+  p.stride[0] = x.k_stride;
+  p.stride[1] = x.v_stride;
+  p.codes[0] = static_cast<uint8_t*>(c.k_codes);
+  p.codes[1] = static_cast<uint8_t*>(c.v_codes);
+  p.scale[0] = static_cast<half_t*>(c.k_scale);
+  p.scale[1] = static_cast<half_t*>(c.v_scale);
+  p.zero[0] = static_cast<half_t*>(c.k_zero);
+  p.zero[1] = static_cast<half_t*>(c.v_zero);
+  p.slots = slots;
+  p.n_tokens = x.n_tokens;
+  p.n_kv_heads = c.n_kv_heads;
+  p.capacity = c.capacity;
+  p.group = c.group_size;
+  p.n_slots = (uint32_t)c.batch * (uint32_t)c.capacity;        // (the caller has checked that it fits)
+  const bool bf16 = x.dtype == TQ_DTYPE_BF16;
+  void (*kernel)(SlotsParams) = nullptr;
+  switch (c.head_dim) {
+    case 128: kernel = bf16 ? quantize_slots_kernel<__bf16, 128> : quantize_slots_kernel<half_t, 128>; break;
+    case 256: kernel = bf16 ? quantize_slots_kernel<__bf16, 256> : quantize_slots_kernel<half_t, 256>; break;
+    case 512: kernel = bf16 ? quantize_slots_kernel<__bf16, 512> : quantize_slots_kernel<half_t, 512>; break;
+    default: return hipErrorInvalidValue;
+  }
+  const int tokens = 256 / (c.head_dim / kGroup);
+  const unsigned blocks = (unsigned)(((int64_t)x.n_tokens + tokens - 1) / tokens);
+  hipLaunchKernelGGL(kernel, dim3(blocks, (unsigned)c.n_kv_heads, 2), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
