@@ -14,8 +14,8 @@ def attend(q, k, v, cu, scale, window=0):
     each; their sum is taken as rounded, so numerator and denominator move by u sum w|v| each at most), the output is rounded (u |o|),
     a score's fp32 sum is off by at most (d + 2) 2^-24 sum |q_i k_i| scale (which moves a weight by as much, relatively, twice that
     with the denominator), an fp32 exp2 and its argument by 2^-22 each, the fp32 sums over n keys by (n + 64) 2^-23 (twice: numerator and denominator; running
-    rescales included).  fp16 weights below 2^-14 are off by 2^-25 at most, absolutely, while the largest of a row is at least 2^-8 (a
-    running maximum may lag behind by a factor of 256): n 2^-17 max|v|.  Outputs below 2^-14 likewise: 2^-25."""
+    rescales included).  fp16 weights below 2^-14 are off by 2^-25 at most, absolutely, where the largest of a row is at least 1: n 2^-25 max|v|,
+    twice with the denominator.  Outputs below 2^-14 likewise: 2^-25."""
     T, hq, d = q.shape
     g = hq // k.shape[1]
     out = torch.zeros((T, hq, d), dtype=torch.float64)
@@ -30,7 +30,7 @@ def attend(q, k, v, cu, scale, window=0):
             w = torch.softmax((qd @ kd.t() * scale).masked_fill(hidden, -math.inf), dim=-1)
             o, spread = w @ vd, w @ vd.abs()
             score = abs(scale) * (d + 2) * 2.0 ** -24 * (qd.abs() @ kd.abs().t()).masked_fill(hidden, 0).amax(-1, keepdim=True)
-            small = (n * 2.0 ** -17 * vd.abs().max() + 2.0 ** -25) if q.dtype == torch.float16 else 0.0
+            small = (n * 2.0 ** -24 * vd.abs().max() + 2.0 ** -25) if q.dtype == torch.float16 else 0.0
             out[a:b, h] = o
             tol[a:b, h] = u * o.abs() + (2 * u + 2 * score + 2.0 ** -20 + (n + 64) * 2.0 ** -22) * spread + small
     return out, tol
