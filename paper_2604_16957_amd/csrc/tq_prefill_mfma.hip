@@ -15,6 +15,7 @@
 #include <cfloat>
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
 #include "tq_internal.h"
 
@@ -68,24 +69,6 @@ __device__ __forceinline__ float add2(uint32_t w, float acc) {
   else return __builtin_amdgcn_fdot2(__builtin_bit_cast(Type<false>::vec2, w), Type<false>::vec2{(_Float16)1.0f, (_Float16)1.0f}, acc, false);
 }
 
-template <int D>
-struct PrefillCfg {
-  // Eight waves, two to a SIMD, share the tiles: one wave's softmax runs beside the other's matrix instructions.  TFLOP/s, 16384 tokens,
-  // 64 heads over 8, d = 128, fp16: eight waves of 32 rows 1023, two blocks of four (which load every tile twice as often) 716, four waves of 64
-  // rows, one to a SIMD, 858.  d = 256, 32 over 16, 8192 tokens, bf16: tiles of 32 keys 1097, of 64 (which spills) 961.
-  static constexpr int NW = 8;                       // waves per block
-  static constexpr int RG = 1;                       // groups of 32 rows per wave
-  static constexpr int ROWS = NW * RG * 32;
-  static constexpr int BN = D == 128 ? 64 : 32;      // keys per tile
-  static constexpr int KS = D / 16;                  // k-steps of the score product
-  static constexpr int DT = D / 32;                  // 32-dim tiles of the output
-  static constexpr int CH = D / 8;                   // 16-byte pieces of a row
-  static constexpr int ROWB = D * 2;
-  static constexpr int TILE = BN * ROWB;
-  static constexpr int LPW = TILE / 1024 / NW;       // 1 KB loads per wave and tile, of K and of V
-  static constexpr int SMEM = 4 * TILE;              // K and V, two tiles each
-};
-
 // Where piece c (16 bytes) of row r lies in an LDS tile.  The score product's operand is read with one row to a lane, the
 // same piece of 32 rows at a time: any 8 consecutive rows have to differ in the banks.  The transposing reads take
 // 64 bytes of four consecutive rows: there the rows have to differ above those 64 bytes.
@@ -98,21 +81,80 @@ __device__ __forceinline__ int v_piece(int r, int c) { return c ^ ((r & 3) << 2)
 __device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(voff), "s"(sbase), "s"(m0) : "memory");
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+template <int N = 0>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }   // until at most N are under way
 __device__ __forceinline__ void block_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// where the row tiles of sequence b start in the list of all (one per sequence is lost at most, none overlap)
+// V^T as the A operand of 16 keys and 32 dims, out of a row-major tile: lane: dim lane % 32, keys 4 hi + 0..3 and 8 + 4 hi + 0..3 (the
+// order in which the scores' accumulator leaves a lane's weights).  The transposing read hands lane i of 16 the i-th of 16 dims that
+// four lanes' addresses name for each of four keys.
+template <int ROWB>
+__device__ __forceinline__ uint32_t v_read(int lane, int d) {    // the lane's offset in a tile, for dims 32 d ...
+  const int r = 4 * (lane >> 5) + (lane & 15) / 4;
+  return r * ROWB + v_piece(r, d * 4 + ((lane >> 4) & 1) * 2 + (lane & 3) / 2) * 16 + (lane & 1) * 8;
+}
+template <bool BF16, int ROWB>
+__device__ __forceinline__ typename Type<BF16>::vec8 v_operand(const char* at) {
+  typedef __attribute__((address_space(3))) short4v* lds_ptr;
+  const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at));
+  const uint2v y = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * ROWB)));
+  return __builtin_bit_cast(typename Type<BF16>::vec8, uint4v{x[0], x[1], y[0], y[1]});
+}
+
+// The same value, which the compiler does not know: what is worked out from it stays where it is used, instead of in registers across the
+// loop.  (Neighbouring LDS offsets of a lane's reads differ in bits that no row's arrangement carries out of: an exclusive or leads
+// from one to the next.)
+__device__ __forceinline__ uint32_t fresh(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// For the scheduler: AHEAD LDS reads, then TIMES matrix instructions with READS reads behind each.  Left alone it puts every read
+// right in front of its use.
+template <int AHEAD>
+__device__ __forceinline__ void order_reads() { __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0); }
+template <int TIMES, int READS>
+__device__ __forceinline__ void order_products() {
+#pragma unroll
+  for (int i = 0; i < TIMES; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+}
+
+// Where the row tiles of sequence b start in the list of all (one per sequence is lost at most, none overlap).  (All tokens have fewer
+// than 2^31 - 256 rows per KV head: a launch has fewer than 2^23 blocks.)
 __device__ __forceinline__ int slot_base(const PrefillParams& p, int b, int rows) {
   const int at = min(max(p.cu_seqlens[b], 0), p.n_tokens);
-  return (int)((int64_t)at * p.gqa / rows) + b;
+  return at * p.gqa / rows + b;
+}
+
+// A row of the output, divided by its sum: 8 dims to a store, for which the wave's halves exchange what they hold of 16.
+template <bool BF16, int DT>
+__device__ __forceinline__ void store_row(uint16_t* dst, const float16v (&o)[DT], float inv, int hi) {
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint32_t x[2], y[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t a = pack2<BF16>(o[d][8 * i + 2 * j] * inv, o[d][8 * i + 2 * j + 1] * inv);
+        const uint32_t b = pack2<BF16>(o[d][8 * i + 4 + 2 * j] * inv, o[d][8 * i + 4 + 2 * j + 1] * inv);
+        const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+        x[j] = r[0];
+        y[j] = r[1];
+      }
+      *reinterpret_cast<uint4v*>(dst + d * 32 + 16 * i + 8 * hi) = uint4v{x[0], x[1], y[0], y[1]};
+    }
 }
 
 // The rows of a slot: `ROWS` consecutive ones of one sequence.
 struct Rows {
   int begin, len;             // the sequence's tokens
-  int64_t tile_row, n_rows;   // the first row (outside of [0, n_rows): nothing to do), and all rows per KV head of the sequence
+  int tile_row, n_rows;       // the first row (outside of [0, n_rows): nothing to do), and all rows per KV head of the sequence
   int t_lo, t_hi;             // first and last of the rows' tokens
 };
 __device__ __forceinline__ Rows find_rows(const PrefillParams& p, int slot, int rows) {
@@ -130,29 +172,36 @@ __device__ __forceinline__ Rows find_rows(const PrefillParams& p, int slot, int 
   Rows r;
   r.begin = min(max(p.cu_seqlens[b], 0), p.n_tokens);
   r.len = min(max(p.cu_seqlens[b + 1], r.begin), p.n_tokens) - r.begin;
-  r.tile_row = (int64_t)(slot - slot_base(p, b, rows)) * rows;
-  r.n_rows = (int64_t)r.len * p.gqa;
-  r.t_lo = (int)(r.tile_row / p.gqa);
-  r.t_hi = (int)(min(r.tile_row + rows - 1, r.n_rows - 1) / p.gqa);
+  r.tile_row = (slot - slot_base(p, b, rows)) * rows;
+  r.n_rows = r.len * p.gqa;
+  r.t_lo = r.tile_row / p.gqa;
+  r.t_hi = min(r.tile_row + rows - 1, r.n_rows - 1) / p.gqa;
   return r;
 }
 
-template <int D, bool BF16>
-__global__ __launch_bounds__(PrefillCfg<D>::NW * 64) void prefill_mfma_kernel(PrefillParams p) {
-  using C = PrefillCfg<D>;
+// ---- head_dim 256
+struct Cfg256 {
+  static constexpr int D = 256, NW = 8, ROWS = NW * 32, BN = 32;     // eight waves, two to a SIMD, share the tiles
+  static constexpr int KS = D / 16, DT = D / 32, CH = D / 8, ROWB = D * 2, TILE = BN * ROWB, LPW = TILE / 1024 / NW;
+  static constexpr int SMEM = 4 * TILE;              // two tiles of K, two of V
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(Cfg256::NW * 64, 2) void prefill256_kernel(PrefillParams p) {
+  using C = Cfg256;
   using T = Type<BF16>;
   using vec8 = typename T::vec8;
-  constexpr int RG = C::RG, NB = C::BN / 32;
+  constexpr int D = C::D;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c32 = lane & 31, hi = lane >> 5;
   const int kv = blockIdx.x % p.n_kv_heads;
   const Rows rows = find_rows(p, p.slots - 1 - (int)(blockIdx.x / p.n_kv_heads), C::ROWS);      // long rows of keys first
   if (rows.tile_row < 0 || rows.tile_row >= rows.n_rows) return;
-  const int begin = rows.begin, len = rows.len, t_lo = rows.t_lo, t_hi = rows.t_hi;
-  const int64_t tile_row = rows.tile_row, n_rows = rows.n_rows;
-  const int first = p.window > 0 ? max(0, t_lo - p.window + 1) : 0;
-  const int n_tiles = (t_hi - first) / C::BN + 1;
+  const int begin = rows.begin, len = rows.len;
+
+  const int first = p.window > 0 ? max(0, rows.t_lo - p.window + 1) : 0;
+  const int n_tiles = (rows.t_hi - first) / C::BN + 1;
   const char* const kb = reinterpret_cast<const char*>(p.k + begin * p.k_stride + (int64_t)kv * D);
   const char* const vb = reinterpret_cast<const char*>(p.v + begin * p.v_stride + (int64_t)kv * D);
   const uint32_t k_row = (uint32_t)p.k_stride * 2, v_row = (uint32_t)p.v_stride * 2;
@@ -160,159 +209,375 @@ __global__ __launch_bounds__(PrefillCfg<D>::NW * 64) void prefill_mfma_kernel(Pr
 
   // Load i of a tile fills the tile's i-th 1024 bytes; its lane fetches the piece that belongs at the lane's place.
   // Rows past the sequence's last token repeat it (finite values that weights of zero meet).
-  auto issue = [&](int tile) {
+  auto issue = [&](const char* base, uint32_t row_bytes, auto piece, int tile, uint32_t to) {
     const int k0 = first + tile * C::BN;
-    const uint32_t to = lds0 + (tile & 1) * (2 * C::TILE);
-    const char* const ks = kb + (int64_t)k0 * k_row;
-    const char* const vs = vb + (int64_t)k0 * v_row;
+    base += (int64_t)k0 * row_bytes;
     const int last = len - 1 - k0;
 #pragma unroll
     for (int u = 0; u < C::LPW; ++u) {
       const int i = u * C::NW + wave;                               // 1 KB pieces go around the waves
       const int r = i * 64 / C::CH + lane / C::CH, c = (i * 64 + lane) % C::CH;
-      const int rr = min(r, last);
-      dma16(ks, (uint32_t)rr * k_row + k_piece(r, c) * 16, to + i * 1024);
-      dma16(vs, (uint32_t)rr * v_row + v_piece(r, c) * 16, to + C::TILE + i * 1024);
+      dma16(base, (uint32_t)min(r, last) * row_bytes + piece(r, c) * 16, to + i * 1024);
     }
   };
-  issue(0);
+  auto issue_k = [&](int tile) { issue(kb, k_row, k_piece, tile, lds0 + (tile & 1) * C::TILE); };
+  auto issue_v = [&](int tile) { issue(vb, v_row, v_piece, tile, lds0 + (2 + (tile & 1)) * C::TILE); };
+  issue_k(0);
 
-  // this lane's rows
-  int token[RG], head[RG];
-  bool mine[RG];
-  vec8 q[RG][C::KS];
-  float16v o[RG][C::DT];
-  float m[RG], l[RG];                                 // log2 units; l: this lane's half of the keys
-#pragma unroll
-  for (int g = 0; g < RG; ++g) {
-    const int64_t row = tile_row + (wave * RG + g) * 32 + c32, my_row = min(row, n_rows - 1);
-    mine[g] = row < n_rows;
-    token[g] = (int)(my_row / p.gqa);
-    head[g] = kv * p.gqa + (int)(my_row - (int64_t)token[g] * p.gqa);
-    const uint16_t* const src = p.q + (begin + token[g]) * p.q_stride + (int64_t)head[g] * D + hi * 8;
+  // this lane's row
+  const int row = rows.tile_row + wave * 32 + c32, my_row = min(row, rows.n_rows - 1);
+  const int token = my_row / p.gqa, head = kv * p.gqa + my_row - token * p.gqa;
+  vec8 q[C::KS];
+  {
+    const uint16_t* const src = p.q + (begin + token) * p.q_stride + (int64_t)head * D + hi * 8;
 #pragma unroll
     for (int s = 0; s < C::KS; ++s) {
       uint4v x = *reinterpret_cast<const uint4v*>(src + s * 16);
       x ^= p.q_flip;
-      q[g][s] = __builtin_bit_cast(vec8, x);
+      q[s] = __builtin_bit_cast(vec8, x);
     }
-#pragma unroll
-    for (int d = 0; d < C::DT; ++d) o[g][d] = float16v{};
-    m[g] = -INFINITY;
-    l[g] = 0.0f;
   }
-  const int w_lo = __builtin_amdgcn_readfirstlane(token[0]);                      // the wave's tokens
-  const int w_hi = __builtin_amdgcn_readlane(token[RG - 1], 31);
+  float16v o[C::DT];
+#pragma unroll
+  for (int d = 0; d < C::DT; ++d) o[d] = float16v{};
+  float m = -INFINITY, l = 0.0f;                      // log2 units; l: this lane's half of the keys
+  const int w_lo = __builtin_amdgcn_readfirstlane(token);                         // the wave's tokens
+  const int w_hi = __builtin_amdgcn_readlane(token, 31);
+  const int oldest = p.window > 0 ? token - p.window + 1 : 0;
 
-  uint32_t k_at[8], v_at[4];                          // LDS offsets of this lane's reads (more pieces, rows: a constant further)
+  const uint32_t k_at0 = c32 * C::ROWB + k_piece(c32, hi) * 16, v_at0 = 2 * C::TILE + v_read<C::ROWB>(lane, 0);   // LDS offsets of this lane's reads
+
+  // tiles that some row of this wave attends
+  const int t_first = p.window > 0 ? max(0, w_lo - p.window + 1 - first) / C::BN : 0, t_last = (w_hi - first) / C::BN;
+
+  float16v s;
+  uint32_t w[8];
+  auto score = [&](int tile) {                        // S^T of a tile
+    const char* const k_lds = smem + (tile & 1) * C::TILE;
+    const uint32_t k_at = fresh(k_at0);
+    s = float16v{};
+#pragma unroll
+    for (int i = 0; i < C::KS; ++i) s = T::mfma(*reinterpret_cast<const vec8*>(k_lds + (k_at ^ ((i & 7) * 32)) + (i >> 3) * 256), q[i], s);
+  };
+  auto weigh = [&](int tile) {                        // masks, maximum, weights
+    const int k0 = first + tile * C::BN;
+    if (k0 + C::BN - 1 > w_lo || (p.window > 0 && k0 <= w_hi - p.window)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = k0 + 8 * (i / 4) + 4 * hi + i % 4;
+        s[i] = key > token || key < oldest ? -INFINITY : s[i];
+      }
+    }
+    float top = s[0], x, y;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    swap32(top, x, y);
+    top = fmaxf(x, y) * p.scale_log2;
+    // The reference may lag behind the maximum by a factor of 2^8 in the weights, which neither the types nor the sums
+    // mind: most tiles then leave the accumulators as they are.
+    if (__any(top > m + 8.0f)) {
+      const float m_new = fmaxf(m, top);
+      const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < C::DT; ++d) o[d] *= alpha;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;      // (no key of this row yet)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], p.scale_log2, -ref));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], p.scale_log2, -ref));
+      w[i] = pack2<BF16>(p0, p1);
+      l = add2<BF16>(w[i], l);
+    }
+  };
+  auto accumulate = [&](int tile) {
+    const char* const v_lds = smem + (tile & 1) * C::TILE;
+    const uint32_t v_at = fresh(v_at0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const vec8 pb = __builtin_bit_cast(vec8, uint4v{w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]});
+#pragma unroll
+      for (int d = 0; d < C::DT; ++d)
+        o[d] = T::mfma(v_operand<BF16, C::ROWB>(v_lds + (v_at ^ ((d & 3) * 64)) + h * 16 * C::ROWB + (d >> 2) * 256), pb, o[d]);
+    }
+  };
+
+  // The two waves of a SIMD take turns: while one is at its matrix instructions (the weights of tile t - 1 meet V, tile t meets
+  // the queries), the other works out its weights.  Left alone they run in step, and the two kinds of work one after the other.
+  // Turns are barriers; waves 0 to 3 have their matrix turn for tile t in turn 2 t, waves 4 to 7 in turn 2 t + 1.  K of tile t is in use in
+  // those two turns and V in the two after; at the start of turn 2 t the next loads begin, and they have two turns.
+  const int off = wave >> 2;
+  auto turn = [&](int i) {
+    if ((i & 1) == 0) wait_loads();
+    block_barrier();
+    if ((i & 1) == 0) {
+      const int t = i >> 1;
+      if (t + 1 < n_tiles) issue_k(t + 1);
+      if (t < n_tiles) issue_v(t);
+    }
+  };
+  int i = 0;
+  while (i < 2 * t_first + off) turn(i++);
+  turn(i++);
+  score(t_first);
+  turn(i++);
+  weigh(t_first);
+  if (t_first < t_last) {
+    int t = t_first;
+    do {
+      turn(i);
+      accumulate(t);
+      score(t + 1);
+      order_reads<6>();
+      order_products<13, 2>();
+      order_products<16, 1>();
+      order_products<3, 0>();
+      turn(i + 1);
+      ++t;
+      i += 2;
+      weigh(t);
+    } while (t < t_last);
+  }
+  turn(i++);
+  accumulate(t_last);
+  while (i < 2 * n_tiles + 2) turn(i++);
+
+  float l0, l1;
+  swap32(l, l0, l1);
+  const float inv = 1.0f / (l0 + l1);                 // (a row has at least its own token)
+  if (row < rows.n_rows) store_row<BF16, C::DT>(p.out + ((int64_t)(begin + token) * p.n_q_heads + head) * D, o, inv, hi);
+}
+
+// ---- head_dim 128
+// Work goes in units of 32 keys, two to a tile.  Of three neighbouring units one is scored, one is weighed and one is accumulated
+// at the same time (step): the three have no dependence on each other, so that the arithmetic of the second fills the issue slots
+// between the matrix instructions of the others.
+struct Cfg128 {
+  static constexpr int D = 128, NW = 4, ROWS = NW * 32, BN = 64;     // two blocks to a compute unit
+  static constexpr int KS = D / 16, DT = D / 32, CH = D / 8, ROWB = D * 2, TILE = BN * ROWB, LPW = TILE / 1024 / NW;
+  static constexpr int SMEM = 4 * TILE;              // two tiles of K, two of V
+};
+// A row's sum of weights from which its reference is brought up to the maximum again.  (fp16 weights are infinite, and so is the
+// sum, from 2^16; both formats keep their precision below.)
+constexpr float kMuch = 0x1p30f;
+
+template <bool BF16>
+__global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillParams p) {
+  using C = Cfg128;
+  using T = Type<BF16>;
+  using vec8 = typename T::vec8;
+  constexpr int D = C::D, NW = C::NW;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c32 = lane & 31, hi = lane >> 5;
+  const int kv = blockIdx.x % p.n_kv_heads;
+  const Rows rows = find_rows(p, p.slots - 1 - (int)(blockIdx.x / p.n_kv_heads), C::ROWS);      // long rows of keys first
+  if (rows.tile_row < 0 || rows.tile_row >= rows.n_rows) return;
+  const int begin = rows.begin, len = rows.len;
+
+  const int first = p.window > 0 ? max(0, rows.t_lo - p.window + 1) : 0;
+  const int n_tiles = (rows.t_hi - first) / C::BN + 1;
+  const uint32_t k_row = (uint32_t)p.k_stride * 2, v_row = (uint32_t)p.v_stride * 2;
+  const char* const kb = reinterpret_cast<const char*>(p.k + (int64_t)(begin + first) * p.k_stride + (int64_t)kv * D);
+  const char* const vb = reinterpret_cast<const char*>(p.v + (int64_t)(begin + first) * p.v_stride + (int64_t)kv * D);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+
+  // Load u of this wave fills 1024 bytes of a tile; a lane fetches the piece that belongs at its place.  Offsets in a whole tile, and
+  // in the last one, where rows past the sequence's last token repeat it (finite values that weights of zero meet).
+  uint32_t k_off[2][C::LPW], v_off[2][C::LPW];
+  {
+    const int last = min(C::BN - 1, len - 1 - first - (n_tiles - 1) * C::BN);
+#pragma unroll
+    for (int u = 0; u < C::LPW; ++u) {
+      const int i = u * NW + wave;                                  // 1 KB pieces go around the waves
+      const int r = i * 64 / C::CH + lane / C::CH, c = (i * 64 + lane) % C::CH;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        k_off[e][u] = (uint32_t)(e ? min(r, last) : r) * k_row + k_piece(r, c) * 16;
+        v_off[e][u] = (uint32_t)(e ? min(r, last) : r) * v_row + v_piece(r, c) * 16;
+      }
+    }
+  }
+  // (past the last tile: the last one again, into a buffer that nobody reads; the count of loads under way is always the same)
+  auto load_k = [&](int tile, int u) {
+    const int t = min(tile, n_tiles - 1);
+    dma16(kb + (int64_t)(t * C::BN) * k_row, t == n_tiles - 1 ? k_off[1][u] : k_off[0][u],
+          lds0 + (tile & 1) * C::TILE + (u * NW + wave) * 1024);
+  };
+  auto load_v = [&](int tile, int u) {
+    const int t = min(tile, n_tiles - 1);
+    dma16(vb + (int64_t)(t * C::BN) * v_row, t == n_tiles - 1 ? v_off[1][u] : v_off[0][u],
+          lds0 + (2 + (tile & 1)) * C::TILE + (u * NW + wave) * 1024);
+  };
+  auto load = [&](int tile) {                        // K of a tile and V of the one before
+#pragma unroll
+    for (int u = 0; u < C::LPW; ++u) {
+      load_k(tile, u);
+      load_v(tile - 1, u);
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < C::LPW; ++u) load_k(0, u);
+
+  // this lane's row
+  const int row = rows.tile_row + wave * 32 + c32, my_row = min(row, rows.n_rows - 1);
+  const int token = my_row / p.gqa, head = kv * p.gqa + my_row - token * p.gqa;
+  vec8 q[C::KS];
+  {
+    const uint16_t* const src = p.q + (begin + token) * p.q_stride + (int64_t)head * D + hi * 8;
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) {
+      uint4v x = *reinterpret_cast<const uint4v*>(src + s * 16);
+      x ^= p.q_flip;
+      q[s] = __builtin_bit_cast(vec8, x);
+    }
+  }
+  float16v o[C::DT];
+#pragma unroll
+  for (int d = 0; d < C::DT; ++d) o[d] = float16v{};
+  float m = -INFINITY, l = 0.0f;                      // log2 units; l: this lane's half of the keys
+  const int w_lo = __builtin_amdgcn_readfirstlane(token), w_hi = __builtin_amdgcn_readlane(token, 31);   // the wave's tokens
+
+  uint32_t k_at[8], v_at[4];                          // LDS offsets of this lane's reads
 #pragma unroll
   for (int i = 0; i < 8; ++i) k_at[i] = c32 * C::ROWB + k_piece(c32, 2 * i + hi) * 16;
 #pragma unroll
-  for (int d = 0; d < 4; ++d) {
-    // Lane: dim 32 d + lane % 32, keys 4 hi + 0..3 and 8 + 4 hi + 0..3 of 16.  The transposing read hands lane i of 16 the i-th
-    // of 16 dims that four lanes' addresses name for each of four keys.
-    const int r = 4 * hi + (lane & 15) / 4;
-    v_at[d] = r * C::ROWB + v_piece(r, d * 4 + ((lane >> 4) & 1) * 2 + (lane & 3) / 2) * 16 + (lane & 1) * 8;
-  }
+  for (int d = 0; d < 4; ++d) v_at[d] = 2 * C::TILE + v_read<C::ROWB>(lane, d);
 
-  for (int tile = 0; tile < n_tiles; ++tile) {
+  // Units that some row of this wave attends; the one by which every row has met a key; the last that no row's own token cuts short
+  const int u_first = p.window > 0 ? max(0, w_lo - p.window + 1 - first) / 32 : 0, u_last = (w_hi - first) / 32;
+  const int u_all = p.window > 0 ? max(0, w_hi - p.window + 1 - first) / 32 : 0;
+  const int u_whole = (w_lo - 31 - first) >> 5;
+  auto active = [&](int u) { return u >= u_first && u <= u_last; };
+
+  typedef uint32_t Weights[8];
+  auto score = [&](float16v& s, int u) {              // S^T of a unit
+    const char* const k_lds = smem + ((u >> 1) & 1) * C::TILE + (u & 1) * (32 * C::ROWB);
+    s = float16v{};
+#pragma unroll
+    for (int i = 0; i < C::KS; ++i) s = T::mfma(*reinterpret_cast<const vec8*>(k_lds + k_at[i]), q[i], s);
+  };
+  auto mask = [&](float16v& s, int u) {               // (key 8 (i / 4) + 4 hi + i % 4 of the unit)
+    const int from = first + u * 32 + 4 * hi, newest = token - from;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 > newest ? -INFINITY : s[i];
+    if (p.window > 0) {
+      const int oldest = newest - p.window + 1;       // (where this wraps, newest < 0 and all of the unit is masked already)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 < oldest ? -INFINITY : s[i];
+    }
+  };
+  auto top_of = [&](const float16v& s) {              // the row's largest score
+    float top = s[0], x, y;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    swap32(top, x, y);
+    return fmaxf(x, y) * p.scale_log2;
+  };
+  auto refer = [&](float top) {                       // the reference becomes the maximum
+    if (!__any(top > m)) return;
+    const float m_new = fmaxf(m, top);
+    const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int d = 0; d < C::DT; ++d) o[d] *= alpha;
+  };
+  auto weigh = [&](const float16v& s, Weights& w) {
+    const float ref = m == -INFINITY ? 0.0f : m;      // (no key of this row yet)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], p.scale_log2, -ref));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], p.scale_log2, -ref));
+      w[i] = pack2<BF16>(p0, p1);
+      l = add2<BF16>(w[i], l);
+    }
+  };
+  auto accumulate = [&](const Weights& w, int u) {
+    const char* const v_lds = smem + ((u >> 1) & 1) * C::TILE + (u & 1) * (32 * C::ROWB);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const vec8 pb = __builtin_bit_cast(vec8, uint4v{w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]});
+#pragma unroll
+      for (int d = 0; d < C::DT; ++d) o[d] = T::mfma(v_operand<BF16, C::ROWB>(v_lds + v_at[d] + h * 16 * C::ROWB), pb, o[d]);
+    }
+  };
+  // Score, weigh and accumulate three units in a row.  The reference stays what it is (a maximum is 8 instructions and an exchange that
+  // all wait for each other) unless the weights show that it lags too far behind.
+  auto step = [&](auto masked, float16v& scored, const float16v& weighed, Weights& w, const Weights& wa, int ua) {
+    const float l_before = l;
+    score(scored, ua + 2);
+    weigh(weighed, w);
+    accumulate(wa, ua);
+    if constexpr (masked) mask(scored, ua + 2);
+    order_reads<6>();
+    order_products<8, 1>();
+    order_products<5, 2>();
+    order_products<3, 0>();
+    if (__any(!(l < kMuch))) {
+      float x, y;
+      swap32(l, x, y);
+      const float over = !(fmaxf(x, y) < kMuch) ? m + 9.0f : -INFINITY;      // (of the row: both halves of the wave)
+      l = l_before;
+      refer(fmaxf(top_of(weighed), over));
+      weigh(weighed, w);
+    }
+  };
+  float16v s0, s1;
+  Weights w0, w1;
+  // Before tile t: unit 2 t is weighed (w0), unit 2 t + 1 scored (s1).  K of tile t + 1 and V of tile t are here, and the loads of K of
+  // tile t + 2 and V of tile t + 1 take the place of what has served.
+  int tile = -1;
+  auto sync = [&]() {
     wait_loads();
     block_barrier();
-    if (tile + 1 < n_tiles) issue(tile + 1);
-    const int k0 = first + tile * C::BN;
-    if (k0 > w_hi || (p.window > 0 && k0 + C::BN - 1 <= w_lo - p.window)) continue;     // nothing here for this wave
-    const char* const k_lds = smem + (tile & 1) * (2 * C::TILE);
-    const char* const v_lds = k_lds + C::TILE;
-    float16v s[RG][NB];
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-#pragma unroll
-      for (int g = 0; g < RG; ++g) s[g][n] = float16v{};
-#pragma unroll
-      for (int i = 0; i < C::KS; ++i) {
-        const vec8 a = *reinterpret_cast<const vec8*>(k_lds + k_at[i & 7] + (n * 32 * C::ROWB + (i >> 3) * 256));
-#pragma unroll
-        for (int g = 0; g < RG; ++g) s[g][n] = T::mfma(a, q[g][i], s[g][n]);
-      }
+  };
+  auto slow = [&]() {
+    sync();
+    load(tile + 2);
+    if (active(2 * tile)) accumulate(w0, 2 * tile);
+    if (active(2 * tile + 1)) {
+      refer(top_of(s1));
+      weigh(s1, w1);
+      accumulate(w1, 2 * tile + 1);
     }
-    if (k0 + C::BN - 1 > w_lo || (p.window > 0 && k0 <= w_hi - p.window)) {
-#pragma unroll
-      for (int g = 0; g < RG; ++g) {
-        const int oldest = p.window > 0 ? token[g] - p.window + 1 : 0;
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = k0 + n * 32 + 8 * (i / 4) + 4 * hi + i % 4;
-            s[g][n][i] = key > token[g] || key < oldest ? -INFINITY : s[g][n][i];
-          }
-      }
+    if (active(2 * tile + 2)) {
+      score(s0, 2 * tile + 2);
+      mask(s0, 2 * tile + 2);
+      refer(top_of(s0));
+      weigh(s0, w0);
     }
-    uint32_t w[RG][NB][8];
-#pragma unroll
-    for (int g = 0; g < RG; ++g) {
-      float top = s[g][0][0];
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[g][n][i]);
-      float a, z;
-      swap32(top, a, z);
-      top = fmaxf(a, z) * p.scale_log2;
-      // The reference may lag behind the maximum by a factor of 2^8 in the weights, which neither the types nor the
-      // sums mind: most tiles then leave the accumulators as they are.
-      if (__any(top > m[g] + 8.0f)) {
-        const float m_new = fmaxf(m[g], top);
-        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[g] - m_new);
-        m[g] = m_new;
-        l[g] *= alpha;
-#pragma unroll
-        for (int d = 0; d < C::DT; ++d) o[g][d] *= alpha;
-      }
-      const float ref = m[g] == -INFINITY ? 0.0f : m[g];        // (no key of this row yet)
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[g][n][2 * i], p.scale_log2, -ref));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[g][n][2 * i + 1], p.scale_log2, -ref));
-          w[g][n][i] = pack2<BF16>(p0, p1);
-          l[g] = add2<BF16>(w[g][n][i], l[g]);
-        }
+    if (active(2 * tile + 3)) {
+      score(s1, 2 * tile + 3);
+      mask(s1, 2 * tile + 3);
     }
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int d = 0; d < C::DT; ++d) {
-          typedef __attribute__((address_space(3))) short4v* lds_ptr;
-          const char* const at = v_lds + v_at[d & 3] + ((n * 32 + h * 16) * C::ROWB + (d >> 2) * 256);
-          const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at));
-          const uint2v y = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * C::ROWB)));
-          const vec8 a = __builtin_bit_cast(vec8, uint4v{x[0], x[1], y[0], y[1]});
-#pragma unroll
-          for (int g = 0; g < RG; ++g) {
-            const vec8 pb = __builtin_bit_cast(vec8, uint4v{w[g][n][4 * h], w[g][n][4 * h + 1], w[g][n][4 * h + 2], w[g][n][4 * h + 3]});
-            o[g][d] = T::mfma(a, pb, o[g][d]);
-          }
-        }
+    ++tile;
+  };
+  // From unit u_all on every row has a reference, and none of its window's start cuts a unit behind that one.
+  while (tile < min((u_all + 1) >> 1, n_tiles)) slow();
+  if (2 * tile + 3 <= u_whole) {
+    do {
+      sync();
+      load(tile + 2);
+      step(std::false_type{}, s0, s1, w1, w0, 2 * tile);
+      step(std::false_type{}, s1, s0, w0, w1, 2 * tile + 1);
+      ++tile;
+    } while (2 * tile + 3 <= u_whole);
   }
-#pragma unroll
-  for (int g = 0; g < RG; ++g) {
-    float l0, l1;
-    swap32(l[g], l0, l1);
-    const float inv = 1.0f / (l0 + l1);                 // (a row has at least its own token)
-    if (!mine[g]) continue;
-    uint16_t* const dst = p.out + ((int64_t)(begin + token[g]) * p.n_q_heads + head[g]) * D;
-#pragma unroll
-    for (int d = 0; d < C::DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint2v x = {pack2<BF16>(o[g][d][4 * i] * inv, o[g][d][4 * i + 1] * inv), pack2<BF16>(o[g][d][4 * i + 2] * inv, o[g][d][4 * i + 3] * inv)};
-        *reinterpret_cast<uint2v*>(dst + d * 32 + 8 * i + 4 * hi) = x;
-      }
+  for (; 2 * tile + 2 <= u_last; ++tile) {
+    sync();
+    load(tile + 2);
+    step(std::true_type{}, s0, s1, w1, w0, 2 * tile);
+    step(std::true_type{}, s1, s0, w0, w1, 2 * tile + 1);
   }
+  while (tile < n_tiles) slow();
+  wait_loads();                                    // (none may arrive after the block's end)
+  float l0, l1;
+  swap32(l, l0, l1);
+  const float inv = 1.0f / (l0 + l1);                 // (a row has at least its own token)
+  if (row < rows.n_rows) store_row<BF16, C::DT>(p.out + ((int64_t)(begin + token) * p.n_q_heads + head) * D, o, inv, hi);
 }
 
 // ---- head_dim 512: a wave can hold neither 32 rows of the output (256 registers) next to their queries (128) at two waves to a
@@ -320,7 +585,7 @@ __global__ __launch_bounds__(PrefillCfg<D>::NW * 64) void prefill_mfma_kernel(Pr
 // B = Q), the weights go through LDS, and it accumulates 128 of the 512 dims over all 64 (32x32 instructions).  K and V have one tile each in
 // LDS: the next K loads while the weights meet V, the next V while K is scored.  The team's maximum is only exchanged where a score
 // passes the one in use by 8 (log2): the waves vote through LDS.
-struct TeamCfg {
+struct Cfg512 {
   static constexpr int D = 512, TEAMS = 2, NW = 4 * TEAMS, ROWS = 32 * TEAMS, BN = 64;
   static constexpr int ROWB = D * 2, TILE = BN * ROWB;
   static constexpr int P_TEAM = 32 * BN * 2;         // weights of a team: [32 rows][64 keys]
@@ -334,8 +599,8 @@ __device__ __forceinline__ float4v mfma16(typename Type<BF16>::vec8 a, typename 
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(TeamCfg::NW * 64, 2) void prefill_team_kernel(PrefillParams p) {
-  using C = TeamCfg;
+__global__ __launch_bounds__(Cfg512::NW * 64, 2) void prefill512_kernel(PrefillParams p) {
+  using C = Cfg512;
   using T = Type<BF16>;
   using vec8 = typename T::vec8;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -346,7 +611,7 @@ __global__ __launch_bounds__(TeamCfg::NW * 64, 2) void prefill_team_kernel(Prefi
   const Rows rows = find_rows(p, p.slots - 1 - (int)(blockIdx.x / p.n_kv_heads), C::ROWS);
   if (rows.tile_row < 0 || rows.tile_row >= rows.n_rows) return;
   const int begin = rows.begin, len = rows.len;
-  const int64_t row0 = rows.tile_row + team * 32;                       // the team's first row
+  const int row0 = rows.tile_row + team * 32;                           // the team's first row
   auto row_at = [&](int i) { return min(row0 + i, rows.n_rows - 1); };
 
   const int first = p.window > 0 ? max(0, rows.t_lo - p.window + 1) : 0;
@@ -355,29 +620,25 @@ __global__ __launch_bounds__(TeamCfg::NW * 64, 2) void prefill_team_kernel(Prefi
   const char* const vb = reinterpret_cast<const char*>(p.v + begin * p.v_stride + (int64_t)kv * C::D);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   // A load is a row; rows past the sequence's last token repeat it.
-  auto issue_k = [&](int tile) {
-#pragma unroll
-    for (int u = 0; u < C::BN / C::NW; ++u) {
-      const int r = u * C::NW + wave;
-      dma16(kb + (int64_t)min(first + tile * C::BN + r, len - 1) * (p.k_stride * 2), k_piece(r, lane) * 16, lds0 + r * C::ROWB);
-    }
+  auto load_k = [&](int tile, int u) {
+    const int r = u * C::NW + wave;
+    dma16(kb + (int64_t)min(first + tile * C::BN + r, len - 1) * (p.k_stride * 2), k_piece(r, lane) * 16, lds0 + r * C::ROWB);
   };
-  auto issue_v = [&](int tile) {
-#pragma unroll
-    for (int u = 0; u < C::BN / C::NW; ++u) {
-      const int r = u * C::NW + wave;
-      dma16(vb + (int64_t)min(first + tile * C::BN + r, len - 1) * (p.v_stride * 2), v_piece(r, lane) * 16, lds0 + C::TILE + r * C::ROWB);
-    }
+  auto load_v = [&](int tile, int u) {
+    const int r = u * C::NW + wave;
+    dma16(vb + (int64_t)min(first + tile * C::BN + r, len - 1) * (p.v_stride * 2), v_piece(r, lane) * 16, lds0 + C::TILE + r * C::ROWB);
   };
-  issue_k(0);
+  constexpr int LPW = C::BN / C::NW;
+#pragma unroll
+  for (int u = 0; u < LPW; ++u) load_k(0, u);
 
   vec8 q[2][16];                                     // rows c16 and c16 + 16
   int token[2];
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
-    const int64_t row = row_at(16 * g + c16);
-    token[g] = (int)(row / p.gqa);
-    const int head = kv * p.gqa + (int)(row - (int64_t)token[g] * p.gqa);
+    const int row = row_at(16 * g + c16);
+    token[g] = row / p.gqa;
+    const int head = kv * p.gqa + row - token[g] * p.gqa;
     const uint16_t* const src = p.q + (begin + token[g]) * p.q_stride + (int64_t)head * C::D + quarter * 8;
 #pragma unroll
     for (int s = 0; s < 16; ++s) {
@@ -393,39 +654,46 @@ __global__ __launch_bounds__(TeamCfg::NW * 64, 2) void prefill_team_kernel(Prefi
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
   float m_out = -INFINITY;                           // the same maximum, of the output's row c32
 
-  uint32_t k_at[4], v_at[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) k_at[i] = (16 * part + c16) * C::ROWB + k_piece(c16, 4 * i + quarter) * 16;
-#pragma unroll
-  for (int d = 0; d < 4; ++d) {
-    const int r = 8 * hi + (lane & 15) / 4;
-    v_at[d] = C::TILE + r * C::ROWB + v_piece(r, d * 4 + ((lane >> 4) & 1) * 2 + (lane & 3) / 2) * 16 + (lane & 1) * 8 + part * 256;
-  }
-  // weights of a row: eight pieces of eight keys, which differ in the banks from row to row
-  char* const p_lds = smem + C::P_AT + team * C::P_TEAM;
+  // LDS offsets of this lane's reads and writes
+  const uint32_t k_at0 = (16 * part + c16) * C::ROWB + k_piece(c16, quarter) * 16;
+  const uint32_t v_at0 = C::TILE + (8 * hi + (lane & 15) / 4) * C::ROWB + v_piece((lane & 15) / 4, ((lane >> 4) & 1) * 2 + (lane & 3) / 2) * 16 +
+                         (lane & 1) * 8 + part * 256;
+  char* const p_lds = smem + C::P_AT + team * C::P_TEAM;                // weights of a row: eight pieces of eight keys
   auto p_at = [&](int row, int piece) { return row * 128 + (piece ^ (row & 7)) * 16; };
-  uint32_t p_wr[2], p_rd[4];
-#pragma unroll
-  for (int g = 0; g < 2; ++g) p_wr[g] = p_at(16 * g + c16, 2 * part + (quarter >> 1)) + (quarter & 1) * 8;
-#pragma unroll
-  for (int s = 0; s < 4; ++s) p_rd[s] = p_at(c32, 2 * s + hi);
+  const uint32_t p_wr0 = p_at(c16, 2 * part + (quarter >> 1)) + (quarter & 1) * 8, p_rd0 = p_at(c32, hi);
   float* const maxima = reinterpret_cast<float*>(smem + C::M_AT) + team * 128;   // [part][row]
-  volatile int* const flags = reinterpret_cast<volatile int*>(smem + C::FLAG_AT);
+  typedef __attribute__((address_space(3))) volatile int lds_int;        // (a generic pointer's accesses would wait for the tile loads)
+  lds_int* const flags = (lds_int*)(smem + C::FLAG_AT);
   if (threadIdx.x < 2) flags[threadIdx.x] = 0;
 
   for (int tile = 0; tile < n_tiles; ++tile) {
     wait_loads();
     block_barrier();                                 // K is here; everybody has done with V
-    issue_v(tile);
     if (threadIdx.x == 0) flags[(tile + 1) & 1] = 0;
     const int k0 = first + tile * C::BN;
     float4v s[2] = {float4v{}, float4v{}};
+    constexpr int kFrags = 2;                        // operands read ahead of their use (four do not fit into the registers)
+    vec8 a[2][kFrags];
+    const uint32_t k_at = fresh(k_at0);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const vec8 a = *reinterpret_cast<const vec8*>(smem + k_at[i & 3] + (i >> 2) * 256);
-      s[0] = mfma16<BF16>(a, q[0][i], s[0]);
-      s[1] = mfma16<BF16>(a, q[1][i], s[1]);
+    for (int i = 0; i < kFrags; ++i) a[0][i] = *reinterpret_cast<const vec8*>(smem + (k_at ^ ((i & 3) * 64)) + (i >> 2) * 256);
+#pragma unroll
+    for (int j = 0; j < 16 / kFrags; ++j) {
+#pragma unroll
+      for (int u = 0; u < LPW * kFrags / 16; ++u) load_v(tile, j * (LPW * kFrags / 16) + u);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < kFrags; ++i) {
+        const int n = (j + 1) * kFrags + i;
+        if (n < 16) a[(j + 1) & 1][i] = *reinterpret_cast<const vec8*>(smem + (k_at ^ ((n & 3) * 64)) + (n >> 2) * 256);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < kFrags; ++i)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) s[g] = mfma16<BF16>(a[j & 1][i], q[g][j * kFrags + i], s[g]);
     }
+    __builtin_amdgcn_sched_barrier(0);
     if (k0 + C::BN - 1 > t_first || (p.window > 0 && k0 <= t_last - p.window)) {
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
@@ -446,7 +714,7 @@ __global__ __launch_bounds__(TeamCfg::NW * 64, 2) void prefill_team_kernel(Prefi
         for (int i = 0; i < 2; ++i)
           w[i] = pack2<BF16>(__builtin_amdgcn_exp2f(fmaf(s[g][2 * i], p.scale_log2, -ref)),
                              __builtin_amdgcn_exp2f(fmaf(s[g][2 * i + 1], p.scale_log2, -ref)));
-        *reinterpret_cast<uint2v*>(p_lds + p_wr[g]) = w;
+        *reinterpret_cast<uint2v*>(p_lds + p_wr0 + g * 2048) = w;
       }
     };
     float top[2];
@@ -460,23 +728,24 @@ __global__ __launch_bounds__(TeamCfg::NW * 64, 2) void prefill_team_kernel(Prefi
     wait_loads();
     block_barrier();                                 // V and the weights are here; everybody has done with K
     if (__builtin_amdgcn_readfirstlane(flags[tile & 1])) {      // (the same answer for the whole block)
+      const int at16 = fresh(c16), at32 = fresh(c32);
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         top[g] = blocks_max(top[g]);
-        if (quarter == 0) maxima[part * 32 + 16 * g + c16] = top[g];
+        if (quarter == 0) maxima[part * 32 + 16 * g + at16] = top[g];
       }
       block_barrier();
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         float m_new = m[g];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) m_new = fmaxf(m_new, maxima[w * 32 + 16 * g + c16]);
+        for (int w = 0; w < 4; ++w) m_new = fmaxf(m_new, maxima[w * 32 + 16 * g + at16]);
         l[g] *= m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[g] - m_new);
         m[g] = m_new;
       }
       float m_new = m_out;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) m_new = fmaxf(m_new, maxima[w * 32 + c32]);
+      for (int w = 0; w < 4; ++w) m_new = fmaxf(m_new, maxima[w * 32 + at32]);
       const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_out - m_new);
       m_out = m_new;
 #pragma unroll
@@ -484,25 +753,31 @@ __global__ __launch_bounds__(TeamCfg::NW * 64, 2) void prefill_team_kernel(Prefi
       weigh();
       block_barrier();
     }
-    if (tile + 1 < n_tiles) issue_k(tile + 1);
+#pragma unroll
+    for (int u = 0; u < LPW; ++u) load_k(min(tile + 1, n_tiles - 1), u);      // (once too often: no branch between here and the products)
 #pragma unroll
     for (int g = 0; g < 2; ++g) {                    // (a wave's own weights, as they lie in LDS)
-      const uint2v w = *reinterpret_cast<const uint2v*>(p_lds + p_wr[g]);
+      const uint2v w = *reinterpret_cast<const uint2v*>(p_lds + p_wr0 + g * 2048);
       l[g] = add2<BF16>(w[1], add2<BF16>(w[0], l[g]));
     }
+    const uint32_t v_at = fresh(v_at0), p_rd = fresh(p_rd0);
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const vec8 pb = *reinterpret_cast<const vec8*>(p_lds + p_rd[n]);
+      const vec8 pb = *reinterpret_cast<const vec8*>(p_lds + (p_rd ^ (n * 32)));
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         typedef __attribute__((address_space(3))) short4v* lds_ptr;
-        const char* const at = smem + v_at[d] + n * 16 * C::ROWB;
+        const char* const at = smem + (v_at ^ (d * 64)) + n * 16 * C::ROWB;
         const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at));
         const uint2v y = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * C::ROWB)));
         o[d] = T::mfma(__builtin_bit_cast(vec8, uint4v{x[0], x[1], y[0], y[1]}), pb, o[d]);
       }
     }
+    order_reads<3 + 8>();
+    order_products<12, 2>();
+    order_products<4, 0>();
   }
+  wait_loads();                                       // (none may arrive after the block's end)
   block_barrier();
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
@@ -510,24 +785,14 @@ __global__ __launch_bounds__(TeamCfg::NW * 64, 2) void prefill_team_kernel(Prefi
     if (quarter == 0) maxima[part * 32 + 16 * g + c16] = sum;
   }
   block_barrier();
-  if (row0 + c32 < rows.n_rows) {
-    const float inv = 1.0f / (maxima[c32] + maxima[32 + c32] + maxima[64 + c32] + maxima[96 + c32]);
-    const int64_t row = row0 + c32;
-    const int tok = (int)(row / p.gqa), head = kv * p.gqa + (int)(row - (int64_t)tok * p.gqa);
-    uint16_t* const dst = p.out + ((int64_t)(begin + tok) * p.n_q_heads + head) * C::D + part * 128;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint2v x = {pack2<BF16>(o[d][4 * i] * inv, o[d][4 * i + 1] * inv), pack2<BF16>(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
-        *reinterpret_cast<uint2v*>(dst + d * 32 + 8 * i + 4 * hi) = x;
-      }
-  }
+  const float inv = 1.0f / (maxima[c32] + maxima[32 + c32] + maxima[64 + c32] + maxima[96 + c32]);
+  const int row = row_at(c32);
+  const int tok = row / p.gqa, head = kv * p.gqa + row - tok * p.gqa;
+  if (row0 + c32 < rows.n_rows)
+    store_row<BF16, 4>(p.out + ((int64_t)(begin + tok) * p.n_q_heads + head) * C::D + part * 128, o, inv, hi);
 }
 
-int block_rows(int head_dim) {
-  return head_dim == 128 ? PrefillCfg<128>::ROWS : head_dim == 256 ? PrefillCfg<256>::ROWS : TeamCfg::ROWS;
-}
+int block_rows(int head_dim) { return head_dim == 128 ? Cfg128::ROWS : head_dim == 256 ? Cfg256::ROWS : Cfg512::ROWS; }
 
 // Launch with so much LDS (over 64 KB: the function has to be told, once per device).
 template <int ID>
@@ -545,10 +810,14 @@ hipError_t launch_kernel(void (*kernel)(PrefillParams), const PrefillParams& p, 
   hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)p.slots * p.n_kv_heads)), dim3(threads), lds, s, p);
   return hipGetLastError();
 }
-template <int D, bool BF16>
-hipError_t launch(const PrefillParams& p, hipStream_t s) {
-  if constexpr (D == 512) return launch_kernel<D + BF16>(prefill_team_kernel<BF16>, p, TeamCfg::NW * 64, TeamCfg::SMEM, s);
-  else return launch_kernel<D + BF16>(prefill_mfma_kernel<D, BF16>, p, PrefillCfg<D>::NW * 64, PrefillCfg<D>::SMEM, s);
+template <bool BF16>
+hipError_t launch(int head_dim, const PrefillParams& p, hipStream_t s) {
+  switch (head_dim) {
+    case 128: return launch_kernel<128 + BF16>(prefill128_kernel<BF16>, p, Cfg128::NW * 64, Cfg128::SMEM, s);
+    case 256: return launch_kernel<256 + BF16>(prefill256_kernel<BF16>, p, Cfg256::NW * 64, Cfg256::SMEM, s);
+    case 512: return launch_kernel<512 + BF16>(prefill512_kernel<BF16>, p, Cfg512::NW * 64, Cfg512::SMEM, s);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace
@@ -579,13 +848,7 @@ hipError_t launch_prefill(const tq_packed_qkv& x, const int32_t* cu_seqlens, int
   p.q_flip = attn_scale < 0 ? 0x80008000u : 0u;
   // (a scale of zero: so small a one that all weights come out as 1, as they should, and that a masked score stays -inf)
   p.scale_log2 = attn_scale == 0.0f ? FLT_MIN : std::fabs(attn_scale) * 1.4426950408889634f;
-  const bool bf16 = x.dtype == TQ_DTYPE_BF16;
-  switch (x.head_dim) {
-    case 128: return bf16 ? launch<128, true>(p, s) : launch<128, false>(p, s);
-    case 256: return bf16 ? launch<256, true>(p, s) : launch<256, false>(p, s);
-    case 512: return bf16 ? launch<512, true>(p, s) : launch<512, false>(p, s);
-    default: return hipErrorInvalidValue;
-  }
+  return x.dtype == TQ_DTYPE_BF16 ? launch<true>(x.head_dim, p, s) : launch<false>(x.head_dim, p, s);
 }
 
 }  // namespace tq
