@@ -469,6 +469,7 @@ class PageState:
         self.n_pages, self.page_tokens = int(free_pages.shape[0]), int(page_tokens)
         self.struct = TqPageStateStruct(seq_lens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), n_free.data_ptr(),
                                         self.batch, self.max_blocks, self.n_pages, self.page_tokens)
+        self.ref, self.device = ctypes.byref(self.struct), seq_lens.device
 
     @classmethod
     def empty(cls, batch: int, max_blocks: int, n_pages: int, page_tokens: int, device="cuda") -> "PageState":
@@ -490,15 +491,23 @@ def _on(device, stream):
 
 def _packed_rows(t: torch.Tensor, name: str, dtype, device) -> int:
     """t: [tokens, heads, head_dim] with a token's heads dense; the elements from one token to the next."""
-    if not t.is_cuda or t.dtype != dtype or t.device != device or dtype not in _DTYPES:
-        raise TypeError(f"{name}: expected a CUDA tensor of float16 or bfloat16, all of one type and device")
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+    if t.dtype != dtype or t.device != device:
+        raise TypeError(f"{name}: expected a tensor of {dtype} on {device}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or stride[2] != 1 or (stride[1] != shape[2] and shape[1] > 1):
         raise ValueError(f"{name}: expected [tokens, heads, head_dim] with a token's heads one after another")
-    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1] * t.shape[2])
+    return stride[0] if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None or not t.is_cuda:
+        raise TypeError("expected CUDA tensors of float16 or bfloat16")
+    return code
 
 
 def _int32s(t: torch.Tensor, name: str, n: int, device):
-    if t.dtype != torch.int32 or t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.device != device or t.numel() != n or t.dim() != 1 or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous int32 tensor of {n} elements on {device}")
 
 
@@ -507,18 +516,21 @@ def tq_sdpa_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlen
     """Causal attention of packed prompts: q fp16 or bf16 [T, H_q, d], k and v [T, H_kv, d] (slices of one fused row are fine),
     cu_seqlens int32 [n_seqs + 1] on the device -> out [T, H_q, d].  Rows that no sequence has are left as they are in `out`
     (undefined in one that the call makes)."""
-    dtype, device = q.dtype, q.device
-    qs, ks, vs = (_packed_rows(t, n, dtype, device) for t, n in ((q, "q"), (k, "k"), (v, "v")))
-    tokens, hq, d = q.shape
-    if k.shape != v.shape or k.shape[0] != tokens or k.shape[2] != d:
+    code, dtype, device = _dtype_code(q), q.dtype, q.device
+    qs, ks, vs = _packed_rows(q, "q", dtype, device), _packed_rows(k, "k", dtype, device), _packed_rows(v, "v", dtype, device)
+    shape = q.shape
+    tokens, hq, d = shape
+    k_tokens, hkv, k_d = k.shape
+    if k_tokens != tokens or k_d != d or v.shape != k.shape:
         raise ValueError("k and v must be [tokens, n_kv_heads, head_dim] of q's tokens and head_dim")
-    _int32s(cu_seqlens, "cu_seqlens", cu_seqlens.numel(), device)
+    n_cu = cu_seqlens.numel()
+    _int32s(cu_seqlens, "cu_seqlens", n_cu, device)
     if out is None:
-        out = torch.empty((tokens, hq, d), dtype=dtype, device=device)
-    elif out.shape != q.shape or out.dtype != dtype or out.device != device or not out.is_contiguous():
+        out = q.new_empty(shape)
+    elif out.shape != shape or out.dtype != dtype or out.device != device or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's shape, type and device")
-    x = TqPackedStruct(q.data_ptr(), k.data_ptr(), v.data_ptr(), qs, ks, vs, tokens, hq, k.shape[1], d, _DTYPES[dtype])
-    rc = raw().tq_sdpa_prefill(ctypes.byref(x), cu_seqlens.data_ptr(), cu_seqlens.numel() - 1, float(attn_scale), int(window),
+    x = TqPackedStruct(q.data_ptr(), k.data_ptr(), v.data_ptr(), qs, ks, vs, tokens, hq, hkv, d, code)
+    rc = raw().tq_sdpa_prefill(ctypes.byref(x), cu_seqlens.data_ptr(), n_cu - 1, float(attn_scale), int(window),
                                out.data_ptr(), _on(device, stream))
     _check(rc, "tq_sdpa_prefill")
     return out
@@ -527,25 +539,25 @@ def tq_sdpa_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlen
 def tq_quantize_kv_slots(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
     """k, v: fp16 or bf16 [T, H_kv, d] (slices of one fused row are fine); slots: int32 [T] on the device, token i goes to row
     slots[i] % capacity of page (or sequence) slots[i] // capacity of the cache; negative: it is not stored."""
-    dtype, device = k.dtype, cache.k_codes.device
+    code, dtype, device = _dtype_code(k), k.dtype, cache.k_codes.device
     ks, vs = _packed_rows(k, "k", dtype, device), _packed_rows(v, "v", dtype, device)
-    tokens, heads, d = k.shape
-    if v.shape != k.shape:
+    tokens, heads, d = shape = k.shape
+    if v.shape != shape:
         raise ValueError("k and v must be of one shape")
     _int32s(slots, "slots", tokens, device)
-    x = TqPackedStruct(None, k.data_ptr(), v.data_ptr(), 0, ks, vs, tokens, 0, heads, d, _DTYPES[dtype])
+    x = TqPackedStruct(None, k.data_ptr(), v.data_ptr(), 0, ks, vs, tokens, 0, heads, d, code)
     rc = raw().tq_quantize_kv_slots(ctypes.byref(cache.struct), ctypes.byref(x), slots.data_ptr(), _on(device, stream))
     _check(rc, "tq_quantize_kv_slots")
 
 
 def _after(state: PageState, seq_lens_after, n_free_after):
     """Where the state goes: the given tensors, or its own."""
+    device = state.device
     lens = state.seq_lens if seq_lens_after is None else seq_lens_after
     free = state.n_free if n_free_after is None else n_free_after
-    device = state.seq_lens.device
-    if lens is not state.seq_lens:
+    if seq_lens_after is not None:
         _int32s(lens, "seq_lens_after", state.batch, device)
-    if free is not state.n_free:
+    if n_free_after is not None:
         _int32s(free, "n_free_after", 1, device)
     return lens.data_ptr(), free.data_ptr(), device
 
@@ -556,22 +568,20 @@ def tq_pages_append(state: PageState, new_lens: torch.Tensor, max_new_tokens: in
     slots [max_new_tokens], served [batch]).  The state's block table gets the new pages; its lengths and free count are brought
     forward in place, or, where seq_lens_after / n_free_after are given, written there."""
     lens, free, device = _after(state, seq_lens_after, n_free_after)
-    _int32s(new_lens, "new_lens", state.batch, device)
-    i32 = dict(dtype=torch.int32, device=device)
-    if cu_seqlens is None:
-        cu_seqlens = torch.empty(state.batch + 1, **i32)
+    batch, max_new_tokens = state.batch, int(max_new_tokens)
+    _int32s(new_lens, "new_lens", batch, device)
+    if cu_seqlens is None and slots is None and served is None and max_new_tokens > 0:   # (one allocation for the three)
+        slots, cu_seqlens, served = new_lens.new_empty(max_new_tokens + 2 * batch + 1).split_with_sizes(
+            (max_new_tokens, batch + 1, batch))
     else:
-        _int32s(cu_seqlens, "cu_seqlens", state.batch + 1, device)
-    if slots is None:
-        slots = torch.empty(max(int(max_new_tokens), 0), **i32)
-    else:
-        _int32s(slots, "slots", int(max_new_tokens), device)
-    if served is None:
-        served = torch.empty(state.batch, **i32)
-    else:
-        _int32s(served, "served", state.batch, device)
-    rc = raw().tq_pages_append(ctypes.byref(state.struct), new_lens.data_ptr(), int(max_new_tokens), lens, free,
-                               cu_seqlens.data_ptr(), slots.data_ptr(), served.data_ptr(), _on(device, stream))
+        cu_seqlens = new_lens.new_empty(batch + 1) if cu_seqlens is None else cu_seqlens
+        slots = new_lens.new_empty(max(max_new_tokens, 0)) if slots is None else slots
+        served = new_lens.new_empty(batch) if served is None else served
+        _int32s(cu_seqlens, "cu_seqlens", batch + 1, device)
+        _int32s(slots, "slots", max_new_tokens, device)
+        _int32s(served, "served", batch, device)
+    rc = raw().tq_pages_append(state.ref, new_lens.data_ptr(), max_new_tokens, lens, free, cu_seqlens.data_ptr(),
+                               slots.data_ptr(), served.data_ptr(), _on(device, stream))
     _check(rc, "tq_pages_append")
     return cu_seqlens, slots, served
 
@@ -580,5 +590,5 @@ def tq_pages_trim(state: PageState, keep_lens: torch.Tensor, seq_lens_after=None
     """Sequence b keeps its first keep_lens[b] tokens (int32 [batch], device); the pages behind them go back on the stack."""
     lens, free, device = _after(state, seq_lens_after, n_free_after)
     _int32s(keep_lens, "keep_lens", state.batch, device)
-    rc = raw().tq_pages_trim(ctypes.byref(state.struct), keep_lens.data_ptr(), lens, free, _on(device, stream))
+    rc = raw().tq_pages_trim(state.ref, keep_lens.data_ptr(), lens, free, _on(device, stream))
     _check(rc, "tq_pages_trim")

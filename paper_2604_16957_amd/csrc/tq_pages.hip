@@ -27,6 +27,7 @@ struct PagesParams {
   int32_t* served;
   int32_t batch, max_blocks, n_pages, page_tokens, bound;   // bound: max_new_tokens
   int32_t outputs, state;     // what this launch writes: everything but the two *_after arrays; those
+  int32_t vector;             // slots is aligned to 16 bytes
 };
 
 constexpr int kThreads = 256, kManyThreads = 1024;
@@ -38,10 +39,14 @@ __device__ __forceinline__ uint32_t add_upto(uint32_t a, uint32_t b, uint32_t mo
 // wave_sums: one word per wave, free again behind the caller's next barrier.
 __device__ inline uint32_t block_scan(uint32_t x, uint32_t most, uint32_t* wave_sums, uint32_t& carry) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  if (!__any(x > (1u << 24))) {                     // (64 of them cannot pass 2^31: plain sums)
+    x = min((uint32_t)wave_scan((int)x), most);
+  } else {
 #pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint32_t y = __shfl_up(x, off);
-    if (lane >= off) x = add_upto(x, y, most);
+    for (int off = 1; off < 64; off <<= 1) {
+      const uint32_t y = __shfl_up(x, off);
+      if (lane >= off) x = add_upto(x, y, most);
+    }
   }
   if (lane == 63) wave_sums[wave] = x;
   __syncthreads();
@@ -68,6 +73,9 @@ __device__ __forceinline__ int first_above(const uint32_t* sums, int n, uint32_t
 
 __device__ __forceinline__ uint32_t pages_of(uint32_t tokens, uint32_t page_tokens) { return (tokens + page_tokens - 1) / page_tokens; }
 
+// RUN: neighbouring tokens (or pages) that a thread takes.  Many tokens: four, mostly of one sequence and page, with one search and one
+// look-up; a decode step has one token to a sequence, and wants a thread for each.
+template <int RUN>
 __global__ __launch_bounds__(kManyThreads) void pages_append_kernel(PagesParams p) {
   extern __shared__ uint32_t lds[];
   uint32_t* const ends = lds;                       // tokens asked for up to and with sequence b, at most bound + 1
@@ -118,17 +126,38 @@ __global__ __launch_bounds__(kManyThreads) void pages_append_kernel(PagesParams 
       const uint32_t held = pages_of((uint32_t)haves[b], P);      // (a page that is taken belongs to a sequence that is served)
       p.table[(int64_t)b * p.max_blocks + held + (j - (b ? takes[b - 1] : 0))] = p.stack[nf - 1 - j];
     }
-    for (uint32_t t = first; t < bound; t += stride) {
-      const int b = first_above(ends, p.batch, t);
-      int32_t slot = -1;
-      if (b < p.batch && haves[b] >= 0) {
-        const uint32_t have = haves[b], pos = have + t - (b ? ends[b - 1] : 0);
-        const uint32_t held = pages_of(have, P), block = pos / P;
-        const int32_t page = block < held ? p.table[(int64_t)b * p.max_blocks + block]
-                                          : p.stack[nf - 1 - ((b ? takes[b - 1] : 0) + block - held)];
-        if ((uint32_t)page < (uint32_t)p.n_pages) slot = page * (int32_t)P + (int32_t)(pos - block * P);
+    for (uint32_t t0 = first * RUN; t0 < bound; t0 += stride * RUN) {
+      int b = first_above(ends, p.batch, t0), of = -1;
+      uint32_t page_at = 0, taken_before = 0, shift = 0;        // of sequence `of`: its page in `page`; pages in front of its; position less token
+      int32_t have = -1, page = -1, slot[RUN];
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) {
+        const uint32_t t = t0 + i;
+        slot[i] = -1;
+        if (RUN > 1) while (b < p.batch && ends[b] <= t) ++b;
+        if (b >= p.batch) continue;
+        bool other = b != of;
+        if (other) {
+          of = b;
+          have = haves[b];
+          shift = (uint32_t)have - (b ? ends[b - 1] : 0);
+          taken_before = b ? takes[b - 1] : 0;
+        }
+        if (have < 0) continue;
+        const uint32_t pos = shift + t, block = pos / P, held = pages_of(have, P);
+        if (other || block != page_at) {
+          page_at = block;
+          page = block < held ? p.table[(int64_t)b * p.max_blocks + block] : p.stack[nf - 1 - (taken_before + block - held)];
+        }
+        if ((uint32_t)page < (uint32_t)p.n_pages) slot[i] = page * (int32_t)P + (int32_t)(pos - block * P);
       }
-      p.slots[t] = slot;
+      if (RUN == 4 && p.vector && t0 + RUN <= bound) {
+        *reinterpret_cast<int4*>(p.slots + t0) = make_int4(slot[0], slot[1 % RUN], slot[2 % RUN], slot[3 % RUN]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < RUN; ++i)
+          if (t0 + i < bound) p.slots[t0 + i] = slot[i];
+      }
     }
   }
   if (p.state && blockIdx.x == 0) {
@@ -140,6 +169,7 @@ __global__ __launch_bounds__(kManyThreads) void pages_append_kernel(PagesParams 
   }
 }
 
+template <int RUN>
 __global__ __launch_bounds__(kManyThreads) void pages_trim_kernel(PagesParams p) {
   extern __shared__ uint32_t lds[];
   uint32_t* const backs = lds;                      // pages given back up to and with sequence b, at most n_pages + 1
@@ -169,9 +199,19 @@ __global__ __launch_bounds__(kManyThreads) void pages_trim_kernel(PagesParams p)
   }
   const uint32_t returned = min(carry, space);
   if (p.outputs) {
-    for (uint32_t j = blockIdx.x * blockDim.x + threadIdx.x; j < returned; j += gridDim.x * blockDim.x) {
-      const int b = first_above(backs, p.batch, j);
-      p.stack[nf + j] = p.table[(int64_t)b * p.max_blocks + lefts[b] + (j - (b ? backs[b - 1] : 0))];
+    const uint32_t stride = gridDim.x * blockDim.x;
+    for (uint32_t j0 = (blockIdx.x * blockDim.x + threadIdx.x) * RUN; j0 < returned; j0 += stride * RUN) {
+      int b = first_above(backs, p.batch, j0);
+      int32_t page[RUN];
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) {
+        const uint32_t j = min(j0 + i, returned - 1);
+        if (RUN > 1) while (backs[b] <= j) ++b;       // (ends: the last sum is more than j)
+        page[i] = p.table[(int64_t)b * p.max_blocks + lefts[b] + (j - (b ? backs[b - 1] : 0))];
+      }
+#pragma unroll
+      for (int i = 0; i < RUN; ++i)
+        if (j0 + i < returned) p.stack[nf + j0 + i] = page[i];
     }
   }
   if (p.state && blockIdx.x == 0) {
@@ -196,10 +236,14 @@ PagesParams params_of(const tq_page_state& st, const int32_t* ask, int32_t* lens
   return p;
 }
 
-// One launch; in place with more than `alone` items, which one block would take long over, two.
-hipError_t launch_pages(void (*kernel)(PagesParams), PagesParams p, int64_t items, int64_t alone, hipStream_t s) {
-  const bool in_place = p.lens_after == p.lens || p.n_free_after == p.n_free;
+// One launch; in place with more than `alone` items, which one block would take long over, two.  us of the kernel, one item to a thread /
+// four: room for a decode step of 256 sequences 4.4 / 6.2, for 90 thousand tokens of prompts 7.8 / 6.2; pages back of 64 sequences that lose a
+// few tokens 2.5 / 3.9, 45 thousand pages 6.6 / 4.8.
+constexpr int64_t kMany = 4096;                     // items from which a thread takes four
+hipError_t launch_pages(void (*kernel)(PagesParams), void (*kernel4)(PagesParams), PagesParams p, int64_t items, int64_t alone, hipStream_t s) {
+  const bool in_place = p.lens_after == p.lens || p.n_free_after == p.n_free, many = items > kMany;
   const size_t lds = (size_t)3 * p.batch * sizeof(uint32_t);
+  if (many) kernel = kernel4;
   p.outputs = 1;
   if (in_place && items <= alone) {
     p.state = 1;
@@ -207,7 +251,8 @@ hipError_t launch_pages(void (*kernel)(PagesParams), PagesParams p, int64_t item
     return hipGetLastError();
   }
   p.state = !in_place;
-  const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>(512, (items + 4 * kThreads - 1) / (4 * kThreads)));
+  const int64_t per_block = kThreads * (many ? 4 : 1);
+  const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>(512, (items + per_block - 1) / per_block));
   hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), lds, s, p);
   if (in_place) {
     const hipError_t rc = hipGetLastError();
@@ -228,13 +273,14 @@ hipError_t launch_pages_append(const tq_page_state& st, const int32_t* new_lens,
   p.slots = slots;
   p.served = served;
   p.bound = max_new_tokens;
-  return launch_pages(pages_append_kernel, p, max_new_tokens, 4096, s);
+  p.vector = (reinterpret_cast<uintptr_t>(slots) & 15) == 0;
+  return launch_pages(pages_append_kernel<1>, pages_append_kernel<4>, p, max_new_tokens, 4096, s);
 }
 
 hipError_t launch_pages_trim(const tq_page_state& st, const int32_t* keep_lens, int32_t* lens_after, int32_t* n_free_after,
                              hipStream_t s) {
   const PagesParams p = params_of(st, keep_lens, lens_after, n_free_after);
-  return launch_pages(pages_trim_kernel, p, std::min<int64_t>((int64_t)st.batch * st.max_blocks, st.n_pages), 16384, s);
+  return launch_pages(pages_trim_kernel<1>, pages_trim_kernel<4>, p, std::min<int64_t>((int64_t)st.batch * st.max_blocks, st.n_pages), 16384, s);
 }
 
 }  // namespace tq
