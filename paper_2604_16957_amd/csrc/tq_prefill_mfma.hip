@@ -124,13 +124,6 @@ __device__ __forceinline__ void order_products() {
   }
 }
 
-// Where the row tiles of sequence b start in the list of all (one per sequence is lost at most, none overlap).  (All tokens have fewer
-// than 2^31 - 256 rows per KV head: a launch has fewer than 2^23 blocks.)
-__device__ __forceinline__ int slot_base(const PrefillParams& p, int b, int rows) {
-  const int at = min(max(p.cu_seqlens[b], 0), p.n_tokens);
-  return at * p.gqa / rows + b;
-}
-
 // A row of the output, divided by its sum: 8 dims to a store, for which the wave's halves exchange what they hold of 16.
 template <bool BF16, int DT>
 __device__ __forceinline__ void store_row(uint16_t* dst, const float16v (&o)[DT], float inv, int hi) {
@@ -158,21 +151,29 @@ struct Rows {
   int t_lo, t_hi;             // first and last of the rows' tokens
 };
 __device__ __forceinline__ Rows find_rows(const PrefillParams& p, int slot, int rows) {
-  const int lane = threadIdx.x & 63;
+  // Where the row tiles of sequence b start in the list of all: one per sequence is lost at most, none overlap.  (All tokens have fewer
+  // than 2^31 - 256 rows per KV head: a launch has fewer than 2^23 blocks.)
+  auto token = [&](int i) { return min(max(p.cu_seqlens[i], 0), p.n_tokens); };
+  auto base = [&](int at, int b) { return at * p.gqa / rows + b; };
   // the last sequence that starts at or before the slot: 64 candidates at a time
-  int b = 0;
-  for (int n = p.n_seqs; n > 1;) {
-    const int step = (n + 63) >> 6, i = lane * step;
-    const bool before = i < n && slot_base(p, b + i, rows) <= slot;
-    const int last = 63 - __clzll((long long)(__ballot(before) | 1));
+  const int lane = threadIdx.x & 63;
+  int b = 0, n = p.n_seqs, begin, end, first_slot;
+  for (;;) {
+    const int step = (n + 63) >> 6, i = b + min(lane * step, n - 1);
+    const int at = token(i), next = token(i + 1);               // (the end counts in the last round, where candidates are neighbours)
+    const int slot_of = base(at, i);
+    const int last = 63 - __clzll((long long)(__ballot(lane * step < n && slot_of <= slot) | 1));
     b += last * step;
     n = min(step, n - last * step);
+    begin = __builtin_amdgcn_readlane(at, last);
+    end = __builtin_amdgcn_readlane(next, last);
+    first_slot = __builtin_amdgcn_readlane(slot_of, last);
+    if (step == 1) break;
   }
-  b = __builtin_amdgcn_readfirstlane(b);
   Rows r;
-  r.begin = min(max(p.cu_seqlens[b], 0), p.n_tokens);
-  r.len = min(max(p.cu_seqlens[b + 1], r.begin), p.n_tokens) - r.begin;
-  r.tile_row = (slot - slot_base(p, b, rows)) * rows;
+  r.begin = begin;
+  r.len = max(end, begin) - begin;
+  r.tile_row = (slot - first_slot) * rows;
   r.n_rows = r.len * p.gqa;
   r.t_lo = r.tile_row / p.gqa;
   r.t_hi = min(r.tile_row + rows - 1, r.n_rows - 1) / p.gqa;
@@ -400,26 +401,17 @@ __global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillP
       }
     }
   }
-  // (past the last tile: the last one again, into a buffer that nobody reads; the count of loads under way is always the same)
-  auto load_k = [&](int tile, int u) {
-    const int t = min(tile, n_tiles - 1);
-    dma16(kb + (int64_t)(t * C::BN) * k_row, t == n_tiles - 1 ? k_off[1][u] : k_off[0][u],
-          lds0 + (tile & 1) * C::TILE + (u * NW + wave) * 1024);
-  };
-  auto load_v = [&](int tile, int u) {
-    const int t = min(tile, n_tiles - 1);
-    dma16(vb + (int64_t)(t * C::BN) * v_row, t == n_tiles - 1 ? v_off[1][u] : v_off[0][u],
-          lds0 + (2 + (tile & 1)) * C::TILE + (u * NW + wave) * 1024);
-  };
-  auto load = [&](int tile) {                        // K of a tile and V of the one before
+  auto load_k = [&](int t) {
 #pragma unroll
-    for (int u = 0; u < C::LPW; ++u) {
-      load_k(tile, u);
-      load_v(tile - 1, u);
-    }
+    for (int u = 0; u < C::LPW; ++u)
+      dma16(kb + (int64_t)(t * C::BN) * k_row, t == n_tiles - 1 ? k_off[1][u] : k_off[0][u], lds0 + (t & 1) * C::TILE + (u * NW + wave) * 1024);
   };
+  auto load_v = [&](int t) {
 #pragma unroll
-  for (int u = 0; u < C::LPW; ++u) load_k(0, u);
+    for (int u = 0; u < C::LPW; ++u)
+      dma16(vb + (int64_t)(t * C::BN) * v_row, t == n_tiles - 1 ? v_off[1][u] : v_off[0][u], lds0 + (2 + (t & 1)) * C::TILE + (u * NW + wave) * 1024);
+  };
+  load_k(0);
 
   // this lane's row
   const int row = rows.tile_row + wave * 32 + c32, my_row = min(row, rows.n_rows - 1);
@@ -533,10 +525,11 @@ __global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillP
   auto sync = [&]() {
     wait_loads();
     block_barrier();
+    if (tile + 2 < n_tiles) load_k(tile + 2);
+    if (tile + 1 < n_tiles) load_v(tile + 1);
   };
   auto slow = [&]() {
     sync();
-    load(tile + 2);
     if (active(2 * tile)) accumulate(w0, 2 * tile);
     if (active(2 * tile + 1)) {
       refer(top_of(s1));
@@ -556,11 +549,23 @@ __global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillP
     ++tile;
   };
   // From unit u_all on every row has a reference, and none of its window's start cuts a unit behind that one.
-  while (tile < min((u_all + 1) >> 1, n_tiles)) slow();
+  if (u_all == 0) {
+    sync();
+    score(s0, 0);
+    score(s1, 1);
+    if (u_whole < 1 || p.window > 0) {
+      mask(s0, 0);
+      mask(s1, 1);
+    }
+    m = fmaxf(top_of(s0), top_of(s1));
+    weigh(s0, w0);
+    tile = 0;
+  } else {
+    while (tile < min((u_all + 1) >> 1, n_tiles)) slow();
+  }
   if (2 * tile + 3 <= u_whole) {
     do {
       sync();
-      load(tile + 2);
       step(std::false_type{}, s0, s1, w1, w0, 2 * tile);
       step(std::false_type{}, s1, s0, w0, w1, 2 * tile + 1);
       ++tile;
@@ -568,7 +573,6 @@ __global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillP
   }
   for (; 2 * tile + 2 <= u_last; ++tile) {
     sync();
-    load(tile + 2);
     step(std::true_type{}, s0, s1, w1, w0, 2 * tile);
     step(std::true_type{}, s1, s0, w0, w1, 2 * tile + 1);
   }
