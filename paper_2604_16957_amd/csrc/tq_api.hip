@@ -704,6 +704,8 @@ int32_t tq_internal_lengths_waves(const tq_kv_cache* cache, int32_t n_q_heads, i
   return waves > 0 ? waves : -chunk_list(cache->batch, cache->n_kv_heads * mfma_share_of(cache, n_q_heads, opts), kBlocksMfma).waves;
 }
 
+int32_t tq_internal_prefill_rows(const tq_packed_qkv* x) { return check_packed(x, true) == TQ_OK ? tq::prefill_block_rows(*x) : 0; }
+
 int32_t tq_internal_counter_sets_left() { return tq::mfma_merge_slots_left(); }
 
 const char* tq_status_string(int status) {

@@ -520,6 +520,7 @@ bool reduce_is_grouped(int head_dim, int64_t out_rows, int n_q_heads, int gqa);
 hipError_t launch_prefill(const tq_packed_qkv& x, const int32_t* cu_seqlens, int n_seqs, float attn_scale, int window, void* out,
                           hipStream_t s);
 int64_t prefill_blocks(const tq_packed_qkv& x, int n_seqs);
+int prefill_block_rows(const tq_packed_qkv& x);
 hipError_t launch_quantize_slots(const tq_kv_cache& c, const tq_packed_qkv& x, const int32_t* slots, hipStream_t s);
 hipError_t launch_pages_append(const tq_page_state& st, const int32_t* new_lens, int32_t max_new_tokens, int32_t* lens_after,
                                int32_t* n_free_after, int32_t* cu_seqlens, int32_t* slots, int32_t* served, hipStream_t s);
@@ -546,6 +547,9 @@ extern "C" int32_t tq_internal_listed_slots(const tq_kv_cache* cache, int32_t n_
 // itself, or, negative, of a slot of the device-planned chunk list; 0 on another kernel.  Not part of the public ABI.
 extern "C" int32_t tq_internal_lengths_waves(const tq_kv_cache* cache, int32_t n_q_heads, int32_t max_seq_len, float attn_scale,
                                              const tq_decode_opts* opts);
+
+// (token, query head) rows of one KV head that a block of tq_sdpa_prefill takes, which tells its instances apart (0: refused); not part of the public ABI.
+extern "C" int32_t tq_internal_prefill_rows(const tq_packed_qkv* x);
 
 // Sets of arrival counters that no workspace has taken yet; not part of the public ABI.
 extern "C" int32_t tq_internal_counter_sets_left();

@@ -181,15 +181,16 @@ __device__ __forceinline__ Rows find_rows(const PrefillParams& p, int slot, int 
 }
 
 // ---- head_dim 256
+template <int NW_>
 struct Cfg256 {
-  static constexpr int D = 256, NW = 8, ROWS = NW * 32, BN = 32;     // eight waves, two to a SIMD, share the tiles
+  static constexpr int D = 256, NW = NW_, ROWS = NW * 32, BN = 32;
   static constexpr int KS = D / 16, DT = D / 32, CH = D / 8, ROWB = D * 2, TILE = BN * ROWB, LPW = TILE / 1024 / NW;
   static constexpr int SMEM = 4 * TILE;              // two tiles of K, two of V
 };
 
-template <bool BF16>
-__global__ __launch_bounds__(Cfg256::NW * 64, 2) void prefill256_kernel(PrefillParams p) {
-  using C = Cfg256;
+template <int NW, bool BF16>
+__global__ __launch_bounds__(NW * 64, 2) void prefill256_kernel(PrefillParams p) {
+  using C = Cfg256<NW>;
   using T = Type<BF16>;
   using vec8 = typename T::vec8;
   constexpr int D = C::D;
@@ -305,15 +306,18 @@ __global__ __launch_bounds__(Cfg256::NW * 64, 2) void prefill256_kernel(PrefillP
     }
   };
 
-  // The two waves of a SIMD take turns: while one is at its matrix instructions (the weights of tile t - 1 meet V, tile t meets
-  // the queries), the other works out its weights.  Left alone they run in step, and the two kinds of work one after the other.
-  // Turns are barriers; waves 0 to 3 have their matrix turn for tile t in turn 2 t, waves 4 to 7 in turn 2 t + 1.  K of tile t is in use in
-  // those two turns and V in the two after; at the start of turn 2 t the next loads begin, and they have two turns.
-  const int off = wave >> 2;
+  // Blocks of eight waves: the two waves of a SIMD take turns.  While one is at its matrix instructions (the weights of tile t - 1
+  // meet V, tile t meets the queries), the other works out its weights; left alone they run in step, and the two kinds of work one after the
+  // other.  Turns are barriers; waves 0 to 3 have their matrix turn for tile t in turn 2 t, waves 4 to 7 in turn 2 t + 1.  K of tile t is in use
+  // in those two turns and V in the two after; at the start of turn 2 t the next loads begin, and they have two turns.  Blocks of four waves
+  // have nobody to take turns with, and a barrier only where the loads want one.
+  const int off = NW == 8 ? wave >> 2 : 0;
   auto turn = [&](int i) {
-    if ((i & 1) == 0) wait_loads();
+    const bool loads = (i & 1) == 0;
+    if (NW == 4 && !loads) return;
+    if (loads) wait_loads();
     block_barrier();
-    if ((i & 1) == 0) {
+    if (loads) {
       const int t = i >> 1;
       if (t + 1 < n_tiles) issue_k(t + 1);
       if (t < n_tiles) issue_v(t);
@@ -796,7 +800,14 @@ __global__ __launch_bounds__(Cfg512::NW * 64, 2) void prefill512_kernel(PrefillP
     store_row<BF16, 4>(p.out + ((int64_t)(begin + tok) * p.n_q_heads + head) * C::D + part * 128, o, inv, hi);
 }
 
-int block_rows(int head_dim) { return head_dim == 128 ? Cfg128::ROWS : head_dim == 256 ? Cfg256::ROWS : Cfg512::ROWS; }
+// head_dim 256: eight waves to a block, which load a tile for twice the rows, where that leaves every compute unit a block and a half at
+// least; else four.  us per call, eight / four, 32 heads over 16, by blocks of eight waves: 54 tokens (16 over 8, 8 blocks) 9.3 / 8.2, 500 (64)
+// 32.3 / 28.5, 8 of 300 (304) 42.1 / 34.2, 2048 (256) 108.3 / 104.8, 4 of 1000 (500) 97.9 / 97.4, 4000 (500) 265 / 272, 4000 of 32 over 4
+// (500) 251 / 266, 8192 (1024) 940 / 997.
+bool wide256(const tq_packed_qkv& x) { return (int64_t)x.n_tokens * x.n_q_heads / Cfg256<8>::ROWS >= 384; }
+int block_rows(const tq_packed_qkv& x) {
+  return x.head_dim == 128 ? Cfg128::ROWS : x.head_dim == 512 ? Cfg512::ROWS : wide256(x) ? Cfg256<8>::ROWS : Cfg256<4>::ROWS;
+}
 
 // Launch with so much LDS (over 64 KB: the function has to be told, once per device).
 template <int ID>
@@ -815,10 +826,12 @@ hipError_t launch_kernel(void (*kernel)(PrefillParams), const PrefillParams& p, 
   return hipGetLastError();
 }
 template <bool BF16>
-hipError_t launch(int head_dim, const PrefillParams& p, hipStream_t s) {
-  switch (head_dim) {
+hipError_t launch(const tq_packed_qkv& x, const PrefillParams& p, hipStream_t s) {
+  switch (x.head_dim) {
     case 128: return launch_kernel<128 + BF16>(prefill128_kernel<BF16>, p, Cfg128::NW * 64, Cfg128::SMEM, s);
-    case 256: return launch_kernel<256 + BF16>(prefill256_kernel<BF16>, p, Cfg256::NW * 64, Cfg256::SMEM, s);
+    case 256:
+      return wide256(x) ? launch_kernel<256 + BF16>(prefill256_kernel<8, BF16>, p, 8 * 64, Cfg256<8>::SMEM, s)
+                        : launch_kernel<258 + BF16>(prefill256_kernel<4, BF16>, p, 4 * 64, Cfg256<4>::SMEM, s);
     case 512: return launch_kernel<512 + BF16>(prefill512_kernel<BF16>, p, Cfg512::NW * 64, Cfg512::SMEM, s);
     default: return hipErrorInvalidValue;
   }
@@ -826,8 +839,10 @@ hipError_t launch(int head_dim, const PrefillParams& p, hipStream_t s) {
 
 }  // namespace
 
+int prefill_block_rows(const tq_packed_qkv& x) { return block_rows(x); }
+
 int64_t prefill_blocks(const tq_packed_qkv& x, int n_seqs) {
-  const int64_t slots = (int64_t)x.n_tokens * (x.n_q_heads / x.n_kv_heads) / block_rows(x.head_dim) + n_seqs;
+  const int64_t slots = (int64_t)x.n_tokens * (x.n_q_heads / x.n_kv_heads) / block_rows(x) + n_seqs;
   return slots * x.n_kv_heads;
 }
 
@@ -852,7 +867,7 @@ hipError_t launch_prefill(const tq_packed_qkv& x, const int32_t* cu_seqlens, int
   p.q_flip = attn_scale < 0 ? 0x80008000u : 0u;
   // (a scale of zero: so small a one that all weights come out as 1, as they should, and that a masked score stays -inf)
   p.scale_log2 = attn_scale == 0.0f ? FLT_MIN : std::fabs(attn_scale) * 1.4426950408889634f;
-  return x.dtype == TQ_DTYPE_BF16 ? launch<true>(x.head_dim, p, s) : launch<false>(x.head_dim, p, s);
+  return x.dtype == TQ_DTYPE_BF16 ? launch<true>(x, p, s) : launch<false>(x, p, s);
 }
 
 }  // namespace tq

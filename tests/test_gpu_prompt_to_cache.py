@@ -1,5 +1,6 @@
 """From a prompt to a paged cache on the GPU: attention of packed prompts, their K and V by slots, pages given and taken back,
 each against its reference in plain Python or 64 bits, and the four of them together in front of decode steps."""
+import ctypes
 import math
 import random
 
@@ -8,7 +9,7 @@ import pytest
 import torch
 
 import paper_2604_16957_amd as tq
-from gpu_common import np16
+from paper_2604_16957_amd import binding as B
 from prompt_common import append, attend, quantize, trim
 
 pytestmark = pytest.mark.gpu
@@ -97,6 +98,23 @@ def test_many_short_sequences():
     lens = [rng.choice([0, 1, 1, 2, 3, 5, 8, 40]) for _ in range(700)]
     q, k, v = _qkv(sum(lens), 8, 1, 128, F16, 9)
     _check_attend(q, k, v, _cu(lens), 0.1)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("window", [0, 40])
+def test_wide_blocks_at_head_dim_256(window, dtype):
+    """Enough rows for blocks of eight waves; and with fewer tokens of the same shape the other instance."""
+    rng = random.Random(5)
+    lens = [rng.choice([1, 31, 64, 65, 130, 200]) for _ in range(40)]
+    lens.append(max(0, 3300 - sum(lens)))
+    q, k, v = _qkv(sum(lens), 32, 4, 256, dtype, 17)
+
+    def rows(T):
+        x = B.TqPackedStruct(q.data_ptr(), k.data_ptr(), v.data_ptr(), 32 * 256, 4 * 256, 4 * 256, T, 32, 4, 256, 0)
+        return B.raw().tq_internal_prefill_rows(ctypes.byref(x))
+
+    assert rows(sum(lens)) == 256 and rows(2000) == 128
+    _check_attend(q, k, v, _cu(lens), 1.0 / 16, window)
 
 
 def test_rows_of_no_sequence_are_left_as_they_were():
