@@ -263,7 +263,7 @@ typedef struct tq_packed_qkv {
  * cu_seqlens: DEVICE int32 [n_seqs + 1], ascending, read by the kernel; sequences may be empty.  Rows of out that no
  * sequence has (before cu_seqlens[0], from cu_seqlens[n_seqs] on) are left as they are.  The values are clamped to
  * [0, n_tokens], so that a bad one gives undefined rows of out but no access outside the arrays.
- * attn_scale: any finite value.  No workspace; one launch.
+ * attn_scale: any finite value (scores, times attn_scale * log2(e), have to stay inside fp32's range).  No workspace; one launch.
  * Errors: NULL, SHAPE, EMPTY (n_tokens or n_seqs < 1), UNSUPPORTED (dtype, window < 0, attn_scale not finite, 2^23
  * blocks or more: n_tokens * n_q_heads / 128 + n_seqs * n_kv_heads), ALIGN, HIP. */
 int tq_sdpa_prefill(const tq_packed_qkv* x, const int32_t* cu_seqlens, int32_t n_seqs, float attn_scale,
