@@ -76,16 +76,48 @@ def test_scales_of_any_sign_and_size(scale, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
-def test_sharp_and_growing_scores(dtype):
-    """Scores that rise with the key (every tile has a new maximum), fall with it, and jump: weights of very different sizes."""
-    n, d = 400, 128
+@pytest.mark.parametrize("d", [128, 256, 512])
+def test_sharp_and_growing_scores(d, dtype):
+    """Scores that rise with the key (every tile has a new maximum), fall with it, jump, or lie far below zero: weights of very
+    different sizes, in heads that see the same keys at different scales and signs side by side."""
+    n = 400
     q, k, v = _qkv(n, 4, 1, d, dtype, 21)
     q[:] = 0
-    q[:, :, 0] = 1.0
-    for shape in (torch.arange(n) * 0.7, -torch.arange(n) * 0.7, torch.where(torch.arange(n) % 97 == 50, 60.0, 0.0), torch.full((n,), -300.0)):
+    q[:, :, 0] = torch.tensor([1.0, 0.03125, -1.0, 0.5], dtype=dtype).cuda()
+    for shape in (torch.arange(n) * 0.75, -torch.arange(n) * 0.75, torch.where(torch.arange(n) % 97 == 50, 60.0, 0.0), torch.full((n,), -300.0)):
         k[:] = 0
         k[:, 0, 0] = shape.to(dtype).cuda()
         _check_attend(q, k, v, [0, n], 1.0)
+        _check_attend(q, k, v, [0, 7, n], 1.0, window=150)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_drawn_shapes(seed):
+    rng = random.Random(100 + seed)
+    d = rng.choice([128, 128, 256, 512])
+    hkv = rng.choice([1, 2, 3])
+    hq = hkv * rng.choice([1, 2, 3, 5, 8, 12])
+    lens = [rng.choice([0, 1, rng.randint(2, 40), rng.randint(40, 700)]) for _ in range(rng.randint(1, 9))] + [5]
+    window = rng.choice([0, 0, 1, rng.randint(2, 300)])
+    dtype = rng.choice([F16, BF16])
+    q, k, v = _qkv(sum(lens), hq, hkv, d, dtype, seed, fused=rng.random() < 0.5)
+    _check_attend(q, k, v, _cu(lens), rng.choice([1.0, 1.0 / math.sqrt(d), -0.05]), window)
+
+
+def test_two_calls_at_once():
+    """Different prompts on two streams, issued in turn and running side by side: no state is shared."""
+    sets = [(_qkv(900, 16, 2, 128, F16, 31), [0, 400, 900]), (_qkv(700, 4, 1, 512, BF16, 32), [0, 1, 700]), (_qkv(800, 8, 4, 256, F16, 33), [0, 800])]
+    cus = [_i32(cu) for _, cu in sets]
+    want = [tq.tq_sdpa_prefill(*x, cu, 0.1) for (x, _), cu in zip(sets, cus)]
+    outs = [[torch.zeros_like(w) for _ in range(4)] for w in want]
+    streams = [torch.cuda.Stream() for _ in sets]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for i in range(4):
+        for (x, _), cu, s, o in zip(sets, cus, streams, outs):
+            tq.tq_sdpa_prefill(*x, cu, 0.1, out=o[i], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for w, several in zip(want, outs) for o in several)
 
 
 def test_a_longer_prompt():
