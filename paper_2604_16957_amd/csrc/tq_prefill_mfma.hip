@@ -674,7 +674,7 @@ __global__ __launch_bounds__(Cfg512::NW * 64, 2) void prefill512_kernel(PrefillP
   const uint32_t v_at0 = C::TILE + (8 * hi + (lane & 15) / 4) * C::ROWB + v_piece((lane & 15) / 4, ((lane >> 4) & 1) * 2 + (lane & 3) / 2) * 16 +
                          (lane & 1) * 8 + part * 256;
   char* const p_lds = smem + C::P_AT + team * C::P_TEAM;                // weights of a row: eight pieces of eight keys
-  auto p_at = [&](int row, int piece) { return row * 128 + (piece ^ (row & 7)) * 16; };
+  auto p_at = [&](int row, int piece) { return row * 128 + (piece ^ ((row >> 1) & 7)) * 16; };   // (two rows to a turn of the banks)
   const uint32_t p_wr0 = p_at(c16, 2 * part + (quarter >> 1)) + (quarter & 1) * 8, p_rd0 = p_at(c32, hi);
   float* const maxima = reinterpret_cast<float*>(smem + C::M_AT) + team * 128;   // [part][row]
   typedef __attribute__((address_space(3))) volatile int lds_int;        // (a generic pointer's accesses would wait for the tile loads)
