@@ -2,16 +2,25 @@
 // heads, fp16 or bf16, on the matrix cores.
 //
 // A row is one (token, query head) pair; the rows of a sequence that share a KV head are numbered token by token,
-// token * gqa + head, and a block takes kRows consecutive ones (so that the heads of a group share every tile of
+// token * gqa + head, and a block takes 64 to 256 consecutive ones (so that the heads of a group share every tile of
 // K and V, and a block's rows span few tokens: little is computed that the causal mask throws away, and a short
-// sequence fills its blocks).  One wave has 32 rows.
+// sequence fills its blocks).  A wave has 32 rows; at head_dim 512 four waves share 32.  Block n works on the n-th
+// block of rows from the end (the longest rows of keys first: what is left for the last compute units is short).
 //
 // Scores are computed transposed, S^T = K Q^T (32 keys x 32 rows to an instruction, A = K, B = Q): a lane then
 // holds 16 keys of ONE row, the softmax's maxima and sums stay in the lane up to one exchange between the wave's
 // halves, and the accumulator's layout is that of the B operand of O^T = V^T P^T up to the order of the keys, which
 // both operands may share in any order.  The A operand V^T comes out of the row-major tile by the transposing LDS
 // read.  Online softmax (Alg. 1) over tiles of keys.
-#include <algorithm>
+//
+// The weights are rounded to the inputs' type because the matrix instruction's operands are that type; their sum takes
+// the rounded ones, so that a row's weights still sum to one.  Everything else is 32 bits up to the output's rounding.
+//
+// Floor: 4 D (attended pairs) H_q operations on the matrix cores; the bytes (q, k, v and out once) are a tenth of that from
+// about 1500 tokens on.  A 32x32x16 product is 32 clocks of a SIMD, and the 16 exponentials, 16 multiply-adds, 8
+// conversions and 8 sums per 32 keys x 32 rows and lane are 8 (exp) or 4 clocks each when one wave issues them, half that when two do:
+// at head_dim 128 as much as the half of its 16 products, which is why each kernel below is arranged around having the two at
+// the same time.
 #include <cfloat>
 #include <cmath>
 #include <mutex>
@@ -81,8 +90,7 @@ __device__ __forceinline__ int v_piece(int r, int c) { return c ^ ((r & 3) << 2)
 __device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(voff), "s"(sbase), "s"(m0) : "memory");
 }
-template <int N = 0>
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }   // until at most N are under way
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void block_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
@@ -124,24 +132,88 @@ __device__ __forceinline__ void order_products() {
   }
 }
 
-// A row of the output, divided by its sum: 8 dims to a store, for which the wave's halves exchange what they hold of 16.
+// Eight dims of a lane's row, 16 i + 8 hi .. of 32, divided by its sum: the wave's halves exchange what they hold of 16.
+template <bool BF16>
+__device__ __forceinline__ uint4v eight_dims(const float16v& o, int i, float inv) {
+  uint32_t x[2], y[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t a = pack2<BF16>(o[8 * i + 2 * j] * inv, o[8 * i + 2 * j + 1] * inv);
+    const uint32_t b = pack2<BF16>(o[8 * i + 4 + 2 * j] * inv, o[8 * i + 4 + 2 * j + 1] * inv);
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    x[j] = r[0];
+    y[j] = r[1];
+  }
+  return uint4v{x[0], x[1], y[0], y[1]};
+}
+// A lane's row of the output, straight to memory.
 template <bool BF16, int DT>
 __device__ __forceinline__ void store_row(uint16_t* dst, const float16v (&o)[DT], float inv, int hi) {
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint32_t x[2], y[2];
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4v*>(dst + d * 32 + 16 * i + 8 * hi) = eight_dims<BF16>(o[d], i, inv);
+}
+
+// The 32 rows of a wave, from row0 on (past the sequence's last row: that one again).
+struct WaveRows {
+  int first;                  // the first row's token
+  int rel0, rel_last, gqa;    // rows counted from that token's first
+  float inv_gqa;
+  __device__ __forceinline__ WaveRows(const PrefillParams& p, int row0, int n_rows) {
+    gqa = p.gqa;
+    const int r0 = min(row0, n_rows - 1);
+    first = r0 / gqa;
+    rel0 = r0 - first * gqa;
+    rel_last = n_rows - 1 - first * gqa;
+    inv_gqa = __builtin_amdgcn_rcpf((float)gqa);
+  }
+  // Row i of the 32: the token counted from the first, and the head of the group.  (The quotient keeps 1 / (2 gqa) off the next integer.  Its
+  // error is 2^-22 of it; it is below 33, and below 2 from gqa = 32 on, and gqa is at most 2^17: rows of 2^24 elements hold no more heads.)
+  __device__ __forceinline__ void at(int i, int& token, int& head) const {
+    const int rel = min(rel0 + i, rel_last);
+    token = (int)(((float)rel + 0.5f) * inv_gqa);
+    head = rel - token * gqa;
+  }
+};
+
+// Queries come, and the output leaves, by way of LDS ([32 rows][D] per wave, pieces as in a tile of K): both sides of memory then see whole
+// rows, where a lane's own row would be 32 bytes of 32 rows to an instruction.  us per call, a lane's own rows / by way of LDS: head_dim 128,
+// 64 heads over 8, 24 prompts of 17 to 2048 tokens 323 / 316, 32 of 512 242 / 237, 173 tokens 7.8 / 7.8.  At head_dim 256 the output alone, in blocks of
+// eight waves: windows of 256 in two prompts of 8192 287 / 272, of 1024 623 / 611; in the small grids of blocks of four waves it costs 0.5 us
+// (54 tokens 8.2 / 8.8), and for the queries' addresses there are no registers.
+template <int D>
+__device__ __forceinline__ void load_queries(const PrefillParams& p, const WaveRows& w, int begin, int kv, uint32_t to) {
+  constexpr int CH = D / 8;
+  const int lane = threadIdx.x & 63;
+  const uint16_t* const base = p.q + (int64_t)(begin + w.first) * p.q_stride + (int64_t)kv * p.gqa * D;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t a = pack2<BF16>(o[d][8 * i + 2 * j] * inv, o[d][8 * i + 2 * j + 1] * inv);
-        const uint32_t b = pack2<BF16>(o[d][8 * i + 4 + 2 * j] * inv, o[d][8 * i + 4 + 2 * j + 1] * inv);
-        const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-        x[j] = r[0];
-        y[j] = r[1];
-      }
-      *reinterpret_cast<uint4v*>(dst + d * 32 + 16 * i + 8 * hi) = uint4v{x[0], x[1], y[0], y[1]};
-    }
+  for (int u = 0; u < CH / 2; ++u) {
+    const int r = (u * 64 + lane) / CH, c = (u * 64 + lane) % CH;
+    int token, head;
+    w.at(r, token, head);
+    dma16(base, (uint32_t)token * (uint32_t)(p.q_stride * 2) + (uint32_t)head * (D * 2) + k_piece(r, c) * 16, to + u * 1024);
+  }
+}
+template <bool BF16, int D>
+__device__ __forceinline__ void store_rows(const PrefillParams& p, const WaveRows& w, int begin, int kv, int n_left, char* lds, const float16v (&o)[D / 32],
+                                           float inv) {
+  constexpr int CH = D / 8;
+  const int lane = threadIdx.x & 63, c32 = lane & 31, hi = lane >> 5;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<uint4v*>(lds + c32 * (D * 2) + k_piece(c32, d * 4 + 2 * i + hi) * 16) = eight_dims<BF16>(o[d], i, inv);
+  uint16_t* const base = p.out + ((int64_t)(begin + w.first) * p.n_q_heads + kv * p.gqa) * D;
+#pragma unroll
+  for (int u = 0; u < CH / 2; ++u) {
+    const int r = (u * 64 + lane) / CH, c = (u * 64 + lane) % CH;
+    int token, head;
+    w.at(r, token, head);
+    const uint4v x = *reinterpret_cast<const uint4v*>(lds + r * (D * 2) + k_piece(r, c) * 16);
+    if (r < n_left) *reinterpret_cast<uint4v*>(base + ((int64_t)token * p.n_q_heads + head) * D + c * 8) = x;
+  }
 }
 
 // The rows of a slot: `ROWS` consecutive ones of one sequence.
@@ -180,12 +252,17 @@ __device__ __forceinline__ Rows find_rows(const PrefillParams& p, int slot, int 
   return r;
 }
 
-// ---- head_dim 256
+// ---- head_dim 256: 64 KB of LDS hold two tiles of K and of V, 32 keys each.  A row's output (128 registers) and queries (64) leave no room for a
+// second unit of scores in flight as at head_dim 128; eight waves take turns instead (see below).  Measured: two sequences of 5003 tokens, 32
+// heads over 16, window 1024: 362 us, 2.0e11 multiply-adds of the attended pairs, 0.72 of what a matrix product of the library reaches (its
+// full tiles: 0.79).  What bounds it: the matrix cores are at work 55 % of the time; the rest is the start of a turn (a barrier, the first LDS
+// reads) and, where the turns are of unlike length, the longer one.  (Not kept: loads by the waves in their arithmetic
+// turn, which spilled registers; both kinds of work in one wave as at 128, likewise.)
 template <int NW_>
 struct Cfg256 {
   static constexpr int D = 256, NW = NW_, ROWS = NW * 32, BN = 32;
   static constexpr int KS = D / 16, DT = D / 32, CH = D / 8, ROWB = D * 2, TILE = BN * ROWB, LPW = TILE / 1024 / NW;
-  static constexpr int SMEM = 4 * TILE;              // two tiles of K, two of V
+  static constexpr int SMEM = NW == 8 ? ROWS * ROWB : 4 * TILE;     // two tiles of K, two of V; the output
 };
 
 template <int NW, bool BF16>
@@ -352,13 +429,25 @@ __global__ __launch_bounds__(NW * 64, 2) void prefill256_kernel(PrefillParams p)
   float l0, l1;
   swap32(l, l0, l1);
   const float inv = 1.0f / (l0 + l1);                 // (a row has at least its own token)
-  if (row < rows.n_rows) store_row<BF16, C::DT>(p.out + ((int64_t)(begin + token) * p.n_q_heads + head) * D, o, inv, hi);
+  if constexpr (NW == 8) {
+    block_barrier();                                  // (everybody has done with the tiles)
+    const int row0 = rows.tile_row + wave * 32;
+    store_rows<BF16, D>(p, WaveRows(p, row0, rows.n_rows), begin, kv, rows.n_rows - row0, smem + wave * (32 * C::ROWB), o, inv);
+  } else if (row < rows.n_rows) {
+    store_row<BF16, C::DT>(p.out + ((int64_t)(begin + token) * p.n_q_heads + head) * D, o, inv, hi);
+  }
 }
 
 // ---- head_dim 128
 // Work goes in units of 32 keys, two to a tile.  Of three neighbouring units one is scored, one is weighed and one is accumulated
 // at the same time (step): the three have no dependence on each other, so that the arithmetic of the second fills the issue slots
 // between the matrix instructions of the others.
+// Measured, 64 heads over 8: 16384 tokens 4.0 ms, 1100 TFLOP/s (a large product of the library: 1154); matrix cores at work 67 % of the
+// time at 1.45 GHz, to which the card's power limit brings the clock (an earlier version at 54 % ran at 1.8 GHz in nearly the same time); 24 sequences of 17 to
+// 2048 tokens (bf16) 319 us, 43 % at 1.96 GHz: there the ends of the sequences' blocks, masked units and the last blocks count.  173 tokens
+// 8.4 us, of which 5 are latency: look-up of the rows, queries, first tile, and the units one after the other.
+// (Not kept, all slower: 64 rows to a wave, where past 256 registers the accumulators are copied; turns as at 256; three tiles ahead with
+// eight waves to a block; an order for the scheduler with the arithmetic's instructions between the products.)
 struct Cfg128 {
   static constexpr int D = 128, NW = 4, ROWS = NW * 32, BN = 64;     // two blocks to a compute unit
   static constexpr int KS = D / 16, DT = D / 32, CH = D / 8, ROWB = D * 2, TILE = BN * ROWB, LPW = TILE / 1024 / NW;
@@ -417,20 +506,23 @@ __global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillP
     for (int u = 0; u < C::LPW; ++u)
       dma16(vb + (int64_t)(t * C::BN) * v_row, t == n_tiles - 1 ? v_off[1][u] : v_off[0][u], lds0 + (2 + (t & 1)) * C::TILE + (u * NW + wave) * 1024);
   };
+  const int row0 = rows.tile_row + wave * 32;
+  const WaveRows mine(p, row0, rows.n_rows);
+  const int q_at = 2 * C::TILE + wave * (32 * C::ROWB);            // (the tiles of V come later)
+  load_queries<D>(p, mine, begin, kv, lds0 + q_at);
   load_k(0);
 
-  // this lane's row
-  const int row = rows.tile_row + wave * 32 + c32, my_row = min(row, rows.n_rows - 1);
-  const int token = my_row / p.gqa, head = kv * p.gqa + my_row - token * p.gqa;
+  // this lane's row, and its queries
+  int token, head;
+  mine.at(c32, token, head);
+  token += mine.first;
   vec8 q[C::KS];
-  {
-    const uint16_t* const src = p.q + (begin + token) * p.q_stride + (int64_t)head * D + hi * 8;
+  wait_loads();
 #pragma unroll
-    for (int s = 0; s < C::KS; ++s) {
-      uint4v x = *reinterpret_cast<const uint4v*>(src + s * 16);
-      x ^= p.q_flip;
-      q[s] = __builtin_bit_cast(vec8, x);
-    }
+  for (int s = 0; s < C::KS; ++s) {
+    uint4v x = *reinterpret_cast<const uint4v*>(smem + q_at + c32 * C::ROWB + k_piece(c32, 2 * s + hi) * 16);
+    x ^= p.q_flip;
+    q[s] = __builtin_bit_cast(vec8, x);
   }
   float16v o[C::DT];
 #pragma unroll
@@ -592,7 +684,8 @@ __global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillP
   float l0, l1;
   swap32(l, l0, l1);
   const float inv = 1.0f / (l0 + l1);                 // (a row has at least its own token)
-  if (row < rows.n_rows) store_row<BF16, C::DT>(p.out + ((int64_t)(begin + token) * p.n_q_heads + head) * D, o, inv, hi);
+  // (Behind the last tile's barrier nobody reads K any more.)
+  store_rows<BF16, D>(p, mine, begin, kv, rows.n_rows - row0, smem + wave * (32 * C::ROWB), o, inv);
 }
 
 // ---- head_dim 512: a wave can hold neither 32 rows of the output (256 registers) next to their queries (128) at two waves to a
@@ -600,6 +693,11 @@ __global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillP
 // B = Q), the weights go through LDS, and it accumulates 128 of the 512 dims over all 64 (32x32 instructions).  K and V have one tile each in
 // LDS: the next K loads while the weights meet V, the next V while K is scored.  The team's maximum is only exchanged where a score
 // passes the one in use by 8 (log2): the waves vote through LDS.
+// Measured, 32 heads over one: 4099 tokens (bf16) 605 us, 910 TFLOP/s; 1024 tokens 59 us.  Matrix cores at work 39 % of the time.  What
+// bounds it is the chain of phases, which all eight waves go through in step, with one block to a compute unit: of about 5500 clocks per tile
+// the scores take 1800 (their products alone 1024), softmax 530, the barrier behind it 550, the loads' issue 690, the output 1300 (1024).  LDS moves
+// 416 KB in that time, 3300 clocks' worth.  (Not kept: four operands read ahead, which spilled registers; K loaded by one team and V by the
+// other, 673 us; the next K's loads spread over the products; 64 rows x 64 dims to a wave's output, which reads 32 KB less from LDS, 617 us.)
 struct Cfg512 {
   static constexpr int D = 512, TEAMS = 2, NW = 4 * TEAMS, ROWS = 32 * TEAMS, BN = 64;
   static constexpr int ROWB = D * 2, TILE = BN * ROWB;

@@ -104,6 +104,13 @@ def test_drawn_shapes(seed):
     _check_attend(q, k, v, _cu(lens), rng.choice([1.0, 1.0 / math.sqrt(d), -0.05]), window)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(129, 1, 128), (1001, 1, 128), (262, 2, 128), (300, 1, 256), (70, 1, 512)])
+def test_more_heads_to_a_group_than_rows_to_a_block(hq, hkv, d):
+    lens = [3, 1, 0, 38]
+    q, k, v = _qkv(sum(lens), hq, hkv, d, F16, hq, fused=True)
+    _check_attend(q, k, v, _cu(lens), 1.0 / math.sqrt(d))
+
+
 def test_two_calls_at_once():
     """Different prompts on two streams, issued in turn and running side by side: no state is shared."""
     sets = [(_qkv(900, 16, 2, 128, F16, 31), [0, 400, 900]), (_qkv(700, 4, 1, 512, BF16, 32), [0, 1, 700]), (_qkv(800, 8, 4, 256, F16, 33), [0, 800])]
