@@ -258,12 +258,15 @@ typedef struct tq_packed_qkv {
 /* Causal attention of whole prompts, before anything of them is quantised.  Sequence b is tokens
  * [cu_seqlens[b], cu_seqlens[b + 1]) of the packed tokens; its token t attends its tokens 0 .. t, with window > 0 the
  * last `window` of them (its own among them).  Query head h reads KV head h / (n_q_heads / n_kv_heads).
- * out: [n_tokens][n_q_heads][head_dim], dense, of the inputs' type; it overlaps none of them.  fp32 scores, softmax and accumulation;
- * the weights are rounded to the inputs' type in front of the product with V (and summed as rounded).
+ * out: [n_tokens][n_q_heads][head_dim], dense, of the inputs' type; it overlaps none of them.  fp32 scores, softmax
+ * and accumulation; the weights are rounded to the inputs' type in front of the product with V (and summed as
+ * rounded).  Infinities and NaN of one sequence stay with that sequence; within it those of V (as weights of zero
+ * times infinity) can reach rows that do not attend their token.
  * cu_seqlens: DEVICE int32 [n_seqs + 1], ascending, read by the kernel; sequences may be empty.  Rows of out that no
  * sequence has (before cu_seqlens[0], from cu_seqlens[n_seqs] on) are left as they are.  The values are clamped to
  * [0, n_tokens], so that a bad one gives undefined rows of out but no access outside the arrays.
- * attn_scale: any finite value (scores, times attn_scale * log2(e), have to stay inside fp32's range).  No workspace; one launch.
+ * attn_scale: any finite value (scores, times attn_scale * log2(e), have to stay inside fp32's range).  No
+ * workspace; one launch.
  * Errors: NULL, SHAPE, EMPTY (n_tokens or n_seqs < 1), UNSUPPORTED (dtype, window < 0, attn_scale not finite, 2^23
  * blocks or more: n_tokens * n_q_heads / 128 + n_seqs * n_kv_heads), ALIGN, HIP. */
 int tq_sdpa_prefill(const tq_packed_qkv* x, const int32_t* cu_seqlens, int32_t n_seqs, float attn_scale,
@@ -272,8 +275,9 @@ int tq_sdpa_prefill(const tq_packed_qkv* x, const int32_t* cu_seqlens, int32_t n
 /* Quantise and store packed tokens (Sec. 2.1, Eq. 2-3), each at a place of its own: token i goes to slot slots[i],
  * i.e. to row slots[i] % capacity of cache row (page, or sequence of a contiguous cache) slots[i] / capacity.
  * slots: DEVICE int32 [n_tokens], read by the kernel; a token whose slot is negative or past the cache
- * is not stored.  Two tokens of a call must not have the same slot.  The same stored bits as tq_quantize_kv gives the same values; from bf16, whose range is wider
- * than the stored fp16, the scale saturates at 65504 (as the zero-point does in any case).  x->q is not read.
+ * is not stored.  Two tokens of a call must not have the same slot.  The stored bits are those of tq_quantize_kv for
+ * the same values; from bf16, whose range is wider than the stored fp16's, the scale saturates at 65504 (as the
+ * zero-point does in any case).  x->q is not read.
  * Any capacity >= 1 (the paged decode calls want a power of two >= 32).
  * Errors: NULL, SHAPE (also x->n_kv_heads or head_dim unlike the cache's), EMPTY (n_tokens < 1),
  * CAPACITY (batch * capacity > 2^31 - 1), UNSUPPORTED (dtype), ALIGN, HIP. */
@@ -297,28 +301,29 @@ typedef struct tq_page_state {
 #define TQ_MAX_PAGED_BATCH 4096
 
 /* Room for new tokens: sequence b asks for new_lens[b] of them (0 or less: none).  In the order of the sequences, each takes
- * the pages that it needs beyond those it holds from the top of the stack.  A sequence is served if its
- * tokens fit into max_blocks pages, lie below max_new_tokens in the packed order, and the stack holds its pages and those of every sequence
- * before it that the first two conditions do not exclude (nobody overtakes a sequence that waits for pages; one that needs none is served all
- * the same).
+ * the pages that it needs beyond those it holds from the top of the stack.  A sequence is served if its tokens fit
+ * into max_blocks pages, lie below max_new_tokens in the packed order, and the stack holds its pages and those of
+ * every sequence before it that the first two conditions do not exclude (nobody overtakes a sequence that waits for
+ * pages; one that needs none is served all the same).
  *   cu_seqlens [batch + 1]: where each sequence's tokens lie in the packed order, served or not, no entry above max_new_tokens;
  *   slots [max_new_tokens]: the slot of every packed token (for tq_quantize_kv_slots): -1 for tokens of a sequence
  *     that is not served, from cu_seqlens[batch] on, and where a page's number is not one of the pool;
  *   served [batch]: 1 or 0 (a sequence that asks for nothing is served as long as what it holds fits);
  *   seq_lens_after [batch], n_free_after [1]: the lengths with the new tokens of the served, and what is left of the
  *     stack.  They may be state->seq_lens and state->n_free themselves: the state is then brought forward in place.
- * state->block_table gets the new pages' entries; state->free_pages is only read.  Negative lengths count as 0, *n_free is
- * clamped to [0, n_pages].  new_lens overlaps no output.
- * One launch, or two (in place, and more than 4096 new tokens).  Errors: NULL, SHAPE, EMPTY (max_new_tokens < 1), CAPACITY
- * (n_pages * page_tokens or max_new_tokens > 2^31 - 2), UNSUPPORTED (batch > TQ_MAX_PAGED_BATCH), ALIGN, HIP. */
+ * state->block_table gets the new pages' entries; state->free_pages is only read.  Negative lengths count as 0,
+ * *n_free is clamped to [0, n_pages].  new_lens overlaps no output.
+ * One launch, or two (in place, and more than 4096 new tokens).  Errors: NULL, SHAPE, EMPTY (max_new_tokens < 1),
+ * CAPACITY (n_pages * page_tokens or max_new_tokens > 2^31 - 2), UNSUPPORTED (batch > TQ_MAX_PAGED_BATCH), ALIGN,
+ * HIP. */
 int tq_pages_append(const tq_page_state* state, const int32_t* new_lens, int32_t max_new_tokens,
                     int32_t* seq_lens_after, int32_t* n_free_after, int32_t* cu_seqlens, int32_t* slots,
                     int32_t* served, void* stream);
 
 /* The way back: sequence b keeps its first keep_lens[b] tokens (0 or less: it is over; its length or more: it stays as it
  * is), and the pages behind them go onto the stack, in the order of the sequences and of their blocks.  Rejected
- * tokens of a speculative step, sequences that end or are preempted.  Entries of the block table are not changed.  Pages that would not fit
- * onto the stack (n_pages entries; the state is then wrong) are dropped.  *_after as above.
+ * tokens of a speculative step, sequences that end or are preempted.  Entries of the block table are not changed.
+ * Pages that would not fit onto the stack (n_pages entries; the state is then wrong) are dropped.  *_after as above.
  * One launch, or two (in place, and more than 16384 entries in the block table).  Errors as above. */
 int tq_pages_trim(const tq_page_state* state, const int32_t* keep_lens, int32_t* seq_lens_after,
                   int32_t* n_free_after, void* stream);

@@ -254,10 +254,11 @@ __device__ __forceinline__ Rows find_rows(const PrefillParams& p, int slot, int 
 
 // ---- head_dim 256: 64 KB of LDS hold two tiles of K and of V, 32 keys each.  A row's output (128 registers) and queries (64) leave no room for a
 // second unit of scores in flight as at head_dim 128; eight waves take turns instead (see below).  Measured: two sequences of 5003 tokens, 32
-// heads over 16, window 1024: 362 us, 2.0e11 multiply-adds of the attended pairs, 0.72 of what a matrix product of the library reaches (its
-// full tiles: 0.79).  What bounds it: the matrix cores are at work 55 % of the time; the rest is the start of a turn (a barrier, the first LDS
-// reads) and, where the turns are of unlike length, the longer one.  (Not kept: loads by the waves in their arithmetic
-// turn, which spilled registers; both kinds of work in one wave as at 128, likewise.)
+// heads over 16, window 1024: 362 us, 830 TFLOP/s, 0.72 of a large product of the library; 8192 tokens without a window 902 us, 1220 TFLOP/s, at
+// the power limit.  What bounds it: a tile takes 3630 clocks where its products alone take 2048 (a barrier and the first LDS reads
+// of every turn), and a block, alone on its compute unit, has about 10 us of start and end (queries 128 KB, output 128 KB) beside 1.7 us per
+// tile.  (Not kept: loads by the waves in their arithmetic turn, and queries by way of LDS, which both spilled registers; both
+// kinds of work in one wave as at 128, likewise; a lane's own row of the output straight to memory, see store_rows.)
 template <int NW_>
 struct Cfg256 {
   static constexpr int D = 256, NW = NW_, ROWS = NW * 32, BN = 32;
@@ -443,8 +444,9 @@ __global__ __launch_bounds__(NW * 64, 2) void prefill256_kernel(PrefillParams p)
 // at the same time (step): the three have no dependence on each other, so that the arithmetic of the second fills the issue slots
 // between the matrix instructions of the others.
 // Measured, 64 heads over 8: 16384 tokens 4.0 ms, 1100 TFLOP/s (a large product of the library: 1154); matrix cores at work 67 % of the
-// time at 1.45 GHz, to which the card's power limit brings the clock (an earlier version at 54 % ran at 1.8 GHz in nearly the same time); 24 sequences of 17 to
-// 2048 tokens (bf16) 319 us, 43 % at 1.96 GHz: there the ends of the sequences' blocks, masked units and the last blocks count.  173 tokens
+// time at 1.4 GHz, to which the card's power limit brings the clock (an earlier version at 54 % ran at 1.8 GHz in nearly the same time); 24 sequences of 17 to
+// 2048 tokens (bf16) 316 us, 43 % at 1.95 GHz: there a block's 41 thousand clocks are 1400 of look-up, 3300 until its queries are there, 2600
+// to the first weights, 2900 per tile, 3400 for the masked tile, 2100 for the end, 2800 to store, and 2300 until the next block has begun.  173 tokens
 // 8.4 us, of which 5 are latency: look-up of the rows, queries, first tile, and the units one after the other.
 // (Not kept, all slower: 64 rows to a wave, where past 256 registers the accumulators are copied; turns as at 256; three tiles ahead with
 // eight waves to a block; an order for the scheduler with the arithmetic's instructions between the products.)
@@ -693,7 +695,7 @@ __global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillP
 // B = Q), the weights go through LDS, and it accumulates 128 of the 512 dims over all 64 (32x32 instructions).  K and V have one tile each in
 // LDS: the next K loads while the weights meet V, the next V while K is scored.  The team's maximum is only exchanged where a score
 // passes the one in use by 8 (log2): the waves vote through LDS.
-// Measured, 32 heads over one: 4099 tokens (bf16) 605 us, 910 TFLOP/s; 1024 tokens 59 us.  Matrix cores at work 39 % of the time.  What
+// Measured, 32 heads over one: 4099 tokens (bf16) 600 to 615 us, 900 TFLOP/s; 1024 tokens 57 us.  Matrix cores at work 39 % of the time.  What
 // bounds it is the chain of phases, which all eight waves go through in step, with one block to a compute unit: of about 5500 clocks per tile
 // the scores take 1800 (their products alone 1024), softmax 530, the barrier behind it 550, the loads' issue 690, the output 1300 (1024).  LDS moves
 // 416 KB in that time, 3300 clocks' worth.  (Not kept: four operands read ahead, which spilled registers; K loaded by one team and V by the
