@@ -268,7 +268,7 @@ typedef struct tq_packed_qkv {
  * attn_scale: any finite value (scores, times attn_scale * log2(e), have to stay inside fp32's range).  No
  * workspace; one launch.
  * Errors: NULL, SHAPE, EMPTY (n_tokens or n_seqs < 1), UNSUPPORTED (dtype, window < 0, attn_scale not finite, 2^23
- * blocks or more: n_tokens * n_q_heads / 128 + n_seqs * n_kv_heads), ALIGN, HIP. */
+ * blocks or more: about n_tokens * n_q_heads / 128, at head_dim 512 / 64, + n_seqs * n_kv_heads), ALIGN, HIP. */
 int tq_sdpa_prefill(const tq_packed_qkv* x, const int32_t* cu_seqlens, int32_t n_seqs, float attn_scale,
                     int32_t window, void* out, void* stream);
 

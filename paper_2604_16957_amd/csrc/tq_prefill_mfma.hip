@@ -168,18 +168,25 @@ struct WaveRows {
     rel_last = n_rows - 1 - first * gqa;
     inv_gqa = __builtin_amdgcn_rcpf((float)gqa);
   }
-  // Row i of the 32: the token counted from the first, and the head of the group.  (The quotient keeps 1 / (2 gqa) off the next integer.  Its
+  // Row i of the 32, counted from the first token's first, and its token, counted from the first.  (The quotient keeps 1 / (2 gqa) off the next integer.  Its
   // error is 2^-22 of it; it is below 33, and below 2 from gqa = 32 on, and gqa is at most 2^17: rows of 2^24 elements hold no more heads.)
-  __device__ __forceinline__ void at(int i, int& token, int& head) const {
-    const int rel = min(rel0 + i, rel_last);
+  __device__ __forceinline__ void at(int i, int& rel, int& token) const {
+    rel = min(rel0 + i, rel_last);
     token = (int)(((float)rel + 0.5f) * inv_gqa);
-    head = rel - token * gqa;
+  }
+  // Bytes from the first token's first row of the KV head to row i, where tokens are `stride` elements apart (fewer than 2^24: 33 of them are
+  // inside 32 bits).
+  template <int D>
+  __device__ __forceinline__ uint32_t bytes(int i, int64_t stride) const {
+    int rel, token;
+    at(i, rel, token);
+    return (uint32_t)rel * (D * 2) + (uint32_t)token * ((uint32_t)stride - (uint32_t)(gqa * D)) * 2;
   }
 };
 
 // Queries come, and the output leaves, by way of LDS ([32 rows][D] per wave, pieces as in a tile of K): both sides of memory then see whole
 // rows, where a lane's own row would be 32 bytes of 32 rows to an instruction.  us per call, a lane's own rows / by way of LDS: head_dim 128,
-// 64 heads over 8, 24 prompts of 17 to 2048 tokens 323 / 316, 32 of 512 242 / 237, 173 tokens 7.8 / 7.8.  At head_dim 256 the output alone, in blocks of
+// 64 heads over 8, 24 prompts of 17 to 2048 tokens 323 / 314, 32 of 512 242 / 237, 2048 79 / 76, 173 7.8 / 7.8.  At head_dim 256 the output alone, in blocks of
 // eight waves: windows of 256 in two prompts of 8192 287 / 272, of 1024 623 / 611; in the small grids of blocks of four waves it costs 0.5 us
 // (54 tokens 8.2 / 8.8), and for the queries' addresses there are no registers.
 template <int D>
@@ -190,9 +197,7 @@ __device__ __forceinline__ void load_queries(const PrefillParams& p, const WaveR
 #pragma unroll
   for (int u = 0; u < CH / 2; ++u) {
     const int r = (u * 64 + lane) / CH, c = (u * 64 + lane) % CH;
-    int token, head;
-    w.at(r, token, head);
-    dma16(base, (uint32_t)token * (uint32_t)(p.q_stride * 2) + (uint32_t)head * (D * 2) + k_piece(r, c) * 16, to + u * 1024);
+    dma16(base, w.bytes<D>(r, p.q_stride) + k_piece(r, c) * 16, to + u * 1024);
   }
 }
 template <bool BF16, int D>
@@ -205,14 +210,12 @@ __device__ __forceinline__ void store_rows(const PrefillParams& p, const WaveRow
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       *reinterpret_cast<uint4v*>(lds + c32 * (D * 2) + k_piece(c32, d * 4 + 2 * i + hi) * 16) = eight_dims<BF16>(o[d], i, inv);
-  uint16_t* const base = p.out + ((int64_t)(begin + w.first) * p.n_q_heads + kv * p.gqa) * D;
+  char* const base = reinterpret_cast<char*>(p.out + ((int64_t)(begin + w.first) * p.n_q_heads + kv * p.gqa) * D);
 #pragma unroll
   for (int u = 0; u < CH / 2; ++u) {
     const int r = (u * 64 + lane) / CH, c = (u * 64 + lane) % CH;
-    int token, head;
-    w.at(r, token, head);
     const uint4v x = *reinterpret_cast<const uint4v*>(lds + r * (D * 2) + k_piece(r, c) * 16);
-    if (r < n_left) *reinterpret_cast<uint4v*>(base + ((int64_t)token * p.n_q_heads + head) * D + c * 8) = x;
+    if (r < n_left) *reinterpret_cast<uint4v*>(base + w.bytes<D>(r, (int64_t)p.n_q_heads * D) + c * 16) = x;
   }
 }
 
@@ -515,8 +518,8 @@ __global__ __launch_bounds__(Cfg128::NW * 64, 2) void prefill128_kernel(PrefillP
   load_k(0);
 
   // this lane's row, and its queries
-  int token, head;
-  mine.at(c32, token, head);
+  int rel, token;
+  mine.at(c32, rel, token);
   token += mine.first;
   vec8 q[C::KS];
   wait_loads();
