@@ -257,7 +257,7 @@ __device__ __forceinline__ Rows find_rows(const PrefillParams& p, int slot, int 
 
 // ---- head_dim 256: 64 KB of LDS hold two tiles of K and of V, 32 keys each.  A row's output (128 registers) and queries (64) leave no room for a
 // second unit of scores in flight as at head_dim 128; eight waves take turns instead (see below).  Measured: two sequences of 5003 tokens, 32
-// heads over 16, window 1024: 362 us, 830 TFLOP/s, 0.72 of a large product of the library; 8192 tokens without a window 902 us, 1220 TFLOP/s, at
+// heads over 16, window 1024: 357 us, 840 TFLOP/s, 0.73 of a large product of the library; 8192 tokens without a window 910 us, 1210 TFLOP/s, at
 // the power limit.  What bounds it: a tile takes 3630 clocks where its products alone take 2048 (a barrier and the first LDS reads
 // of every turn), and a block, alone on its compute unit, has about 10 us of start and end (queries 128 KB, output 128 KB) beside 1.7 us per
 // tile.  (Not kept: loads by the waves in their arithmetic turn, and queries by way of LDS, which both spilled registers; both
